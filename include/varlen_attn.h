@@ -236,6 +236,76 @@ va_status va_varlen_attn_bwd_stages(const void *dO, const void *Q, const void *K
                                     va_dtype dt, float softmax_scale, void *workspace,
                                     size_t workspace_bytes, void *stream, uint32_t stages);
 
+/*
+ * Key-value cache.  What a model that generates does after a packed stream of prompts has gone through the calls above: K and V
+ * of the prompts' tokens are kept in pages, and one new token of every sequence at a time attends to them.
+ *
+ * The pages belong to the caller, who hands them out; a page holds page_size consecutive tokens of one sequence, all KV heads.
+ *   k, v             : device, [n_pages, hkv, page_size, d], 16-byte aligned for full speed.
+ *   k_scale, v_scale : device, [n_pages, hkv, page_size] float, of the 8-bit formats (unused, may be NULL, otherwise): a cached
+ *                      element stands for its value times the scale of its token and head.
+ *   page_table       : device, [n_seqs] rows of max_pages int32, table_stride entries apart: position p of sequence s lies in
+ *                      page page_table[s * table_stride + p / page_size], at place p % page_size.  An entry outside
+ *                      [0, n_pages) is no page; sequences may share pages.
+ * Limits: n_pages * hkv * page_size < 2^31 (rows of one tensor), max_pages * page_size < 2^31, page_size * d < 2^26, n_seqs <= 65535.
+ */
+typedef enum {
+  VA_CACHE_PLAIN = 0, /* elements of the type that the call names for K and V (or Q)            */
+  VA_CACHE_I8 = 1,    /* int8 integers, at most 127 in magnitude                                   */
+  VA_CACHE_E4M3 = 2   /* 8-bit floats, 4 exponent and 3 mantissa bits, no infinity, at most 448    */
+} va_cache_format;
+
+typedef struct va_kv_cache {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t n_pages, page_size, hkv, d;
+  va_cache_format format;
+  int32_t n_seqs, max_pages;
+  int64_t table_stride;
+  const int32_t *page_table;
+} va_kv_cache;
+
+/*
+ * Rows of K and V into the cache.  Token t belongs to sequence seq_ids[t] (t itself where seq_ids is NULL: one new token of
+ * every sequence) and to position position_ids[t] there; a packed stream of prompts brings its position ids and seg_id.
+ *   K, V         : device, [n_tokens, hkv, d] of `dt`.
+ *   seq_ids      : device, [n_tokens] int32, or NULL.
+ *   position_ids : device, [n_tokens] of `it`.
+ * A token without a place (a sequence outside [0, n_seqs), a position outside [0, max_pages * page_size), an entry that is no
+ * page) is left out: the padding behind a packed row, whose seg_id is one more than the last sequence's, needs no care.  All
+ * other rows of the cache stay as they are.  Of several tokens with one place any one's elements may be stored, of each row
+ * piece by piece; identical rows (a prefix that sequences share) are safe.
+ * 8-bit formats: per token and head a = max_c |x_c|, scale = a / m, and x_c is stored as m x_c / a rounded to nearest even,
+ * m = 127 or 448; exactly for 16-bit rows.  a = 0: all zeros.  A row that holds a NaN or an infinity gets the scale NaN.
+ */
+va_status va_cache_write(const void *K, const void *V, va_dtype dt, const va_kv_cache *cache, const int32_t *seq_ids,
+                         const void *position_ids, va_itype it, int32_t n_tokens, void *stream);
+
+/*
+ * Rows of the cache as a packed stream: the inverse of the above, K and V [n_tokens, hkv, d] of `dt` (format PLAIN: the type
+ * that was written), 8-bit elements times their scale in fp32 and rounded once.  Tokens without a place become zeros.
+ */
+va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache, const int32_t *seq_ids,
+                        const void *position_ids, va_itype it, int32_t n_tokens, void *stream);
+
+/*
+ * One new token of every sequence attends to what the cache holds of it: with context_lens[s] = n, head h and its KV head,
+ *     S_j = softmax_scale * q . k_j  (0 <= j < n),  P = softmax_j(S),  O = sum_j P_j v_j,  LSE = log sum_j exp(S_j)
+ * (row n - 1 of va_varlen_attn_fwd over the whole sequence, where the token's own K and V are already written).
+ *   Q, O          : device, [n_seqs, hq, d] of `dt`; hq a multiple of the cache's hkv, d its d.
+ *   LSE           : device, [hq, n_seqs] float.
+ *   context_lens  : device, [n_seqs] int32, clamped to [0, max_pages * page_size].  Positions whose table entry is no page are
+ *                   left out.  A sequence of which nothing is left: O = 0, LSE = -infinity.
+ *   softmax_scale : <= 0 means 1 / sqrt(d).
+ *   workspace     : >= va_paged_attn_workspace_bytes(...) bytes (may be NULL when that is 0): sums of the parts that long
+ *                   sequences are cut into.  Calls that overlap in time need one each.
+ * The parts follow from the lengths alone and are joined in order: results are deterministic (no atomics).
+ */
+size_t va_paged_attn_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t page_size, int32_t hq, int32_t hkv, int32_t d);
+va_status va_paged_attn_fwd(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache *cache, int32_t hq,
+                            const int32_t *context_lens, float softmax_scale, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
 /* Static string for a status code. */
 const char *va_status_string(va_status s);
 

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import logging
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -27,18 +27,26 @@ VA_I32, VA_I64 = 0, 1
 VA_TILE = 256
 STAGE_D, STAGE_DKDV, STAGE_DQ = 1, 2, 4
 HINT_LONG_EXAMPLES, HINT_SHORT_EXAMPLES = 8, 16
+CACHE_PLAIN, CACHE_I8, CACHE_E4M3 = 0, 1, 2
 
 EXPORTS = (
     "va_plan_bytes", "va_segments_bind", "va_pack_to_cu_seqlens", "va_attn_workspace_bytes",
     "va_varlen_attn_fwd", "va_varlen_attn_bwd", "va_varlen_attn_bwd_stages", "va_varlen_attn_bwd_noalloc",
     "va_collate_padding_free",
-    "va_rope_apply", "va_status_string", "va_version",
+    "va_rope_apply", "va_cache_write", "va_cache_read", "va_paged_attn_workspace_bytes", "va_paged_attn_fwd",
+    "va_status_string", "va_version",
 )
 
 
 class VaSegments(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in (
         "cu_seqlens", "seg_id", "seg_start", "seg_end", "meta", "q_tile_order", "kv_tile_order", "scratch")]
+
+
+class VaKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("hkv", C.c_int32), ("d", C.c_int32), ("format", C.c_int),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("table_stride", C.c_int64), ("page_table", C.c_void_p)]
 
 
 _lib = None
@@ -81,6 +89,14 @@ def lib() -> C.CDLL:
     L.va_rope_apply.restype = C.c_int
     L.va_rope_apply.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int32, C.c_int32,
                                 C.c_int32, C.c_float, C.c_int, C.c_void_p]
+    for f in (L.va_cache_write, L.va_cache_read):
+        f.restype = C.c_int
+        f.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.POINTER(VaKvCache), C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_void_p]
+    L.va_paged_attn_workspace_bytes.restype = C.c_size_t
+    L.va_paged_attn_workspace_bytes.argtypes = [C.c_int32] * 6
+    L.va_paged_attn_fwd.restype = C.c_int
+    L.va_paged_attn_fwd.argtypes = [C.c_void_p] * 3 + [C.c_int, C.POINTER(VaKvCache), C.c_int32, C.c_void_p, C.c_float,
+                                    C.c_void_p, C.c_size_t, C.c_void_p]
     L.va_status_string.restype = C.c_char_p
     L.va_status_string.argtypes = [C.c_int]
     L.va_version.restype = C.c_char_p
@@ -410,3 +426,139 @@ def varlen_attn_bwd_noalloc(do, q, k, v, o, lse, seg: Segments, dq, dk, dv, soft
         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _dt(dq), C.byref(seg.c), seg.rows, seg.tokens_per_row,
         hq, hkv, d, _dt(q), float(softmax_scale), _stream()))
     return dq, dk, dv
+
+
+# ---- key-value cache ----------------------------------------------------------------------------------
+
+
+class PagedCache(NamedTuple):
+    """Pages of cached keys and values: k, v [n_pages, Hkv, page_size, d]; k_scale, v_scale [n_pages, Hkv, page_size] float32 where
+    the elements are int8 or float8_e4m3fn, else None.  The calls below take any such four tensors as a tuple."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+_CACHE_FORMATS = {torch.float32: CACHE_PLAIN, torch.bfloat16: CACHE_PLAIN, torch.float16: CACHE_PLAIN, torch.int8: CACHE_I8,
+                  torch.float8_e4m3fn: CACHE_E4M3}
+
+
+def paged_cache(n_pages: int, page_size: int, hkv: int, d: int, dtype: torch.dtype, device="cuda") -> PagedCache:
+    """An empty cache (zeros).  dtype: that of K and V, or int8 or float8_e4m3fn, whose rows also carry a float32 scale."""
+    if dtype not in _CACHE_FORMATS:
+        raise TypeError(f"unsupported cache dtype {dtype}")
+    pages = [torch.zeros((n_pages, hkv, page_size, d), dtype=dtype, device=device) for _ in "kv"]
+    scales = [torch.zeros((n_pages, hkv, page_size), dtype=torch.float32, device=device) for _ in "kv"
+              if _CACHE_FORMATS[dtype] != CACHE_PLAIN]
+    return PagedCache(*pages, *scales)
+
+
+def _kv_cache(cache, page_table: torch.Tensor, dtype: torch.dtype, *others) -> VaKvCache:
+    """The library's view of a cache and the pages of a call's sequences, for rows (or queries) of `dtype`; the call's tensors, `others`
+    among them, must live on the current device."""
+    k, v, k_scale, v_scale = cache
+    _need_cuda(k, v, *others)
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("expected cache pages k, v [n_pages, Hkv, page_size, d] of one dtype")
+    fmt = _CACHE_FORMATS.get(k.dtype)
+    if fmt is None or (fmt == CACHE_PLAIN and k.dtype != dtype):
+        raise TypeError(f"a cache of {k.dtype} does not serve {dtype}")
+    tensors = [k, v, page_table, *others]
+    if fmt != CACHE_PLAIN:
+        for name, scale in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if scale is None:
+                raise ValueError(f"a cache of {k.dtype} needs {name}")
+            _out_like(name, scale, k.shape[:3], torch.float32, k.device)
+    if not page_table.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32:
+        raise ValueError("page_table must be int32 [sequences, pages]")
+    seqs, width = page_table.shape
+    stride = page_table.stride(0) if seqs > 1 else width
+    if (width > 1 and page_table.stride(1) != 1) or stride < width:
+        raise ValueError("the entries of a sequence must lie next to each other in page_table, and sequences apart")
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != here:
+            raise ValueError(f"a tensor lives on {t.device}, the current device is cuda:{here}")
+    scales = (None, None) if fmt == CACHE_PLAIN else (k_scale.data_ptr(), v_scale.data_ptr())
+    n_pages, hkv, page_size, d = k.shape
+    return VaKvCache(k.data_ptr(), v.data_ptr(), *scales, n_pages, page_size, hkv, d, fmt, seqs, width, stride, page_table.data_ptr())
+
+
+def _cache_rows(k, v, cache, page_table, position_ids, seq_ids):
+    """Checks what a write and a read have in common; -> the cache's view and the library's arguments from dtype to n_tokens."""
+    more = () if seq_ids is None else (seq_ids,)
+    c = _kv_cache(cache, page_table, k.dtype, k, v, position_ids, *more)
+    if k.dim() != 3 or v.shape != k.shape or v.dtype != k.dtype or k.shape[1:] != (c.hkv, c.d):
+        raise ValueError(f"expected K, V [N, {c.hkv}, {c.d}] of one dtype")
+    N = k.shape[0]
+    if position_ids.numel() != N or position_ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"expected {N} position ids, int32 or int64")
+    if seq_ids is not None and (seq_ids.numel() != N or seq_ids.dtype != torch.int32):
+        raise ValueError(f"expected {N} int32 sequence ids")
+    return (_dt(k), C.byref(c), None if seq_ids is None else seq_ids.data_ptr(), position_ids.data_ptr(),
+            VA_I64 if position_ids.dtype == torch.int64 else VA_I32, N)
+
+
+def paged_cache_write(k: torch.Tensor, v: torch.Tensor, cache, page_table: torch.Tensor, position_ids: torch.Tensor,
+                      seq_ids: Optional[torch.Tensor] = None) -> None:
+    """K and V rows [N, Hkv, d] into the pages of their sequences: token t is token position_ids[t] (N entries, int32 or int64) of
+    sequence seq_ids[t] (int32; default: t), whose pages are row seq_ids[t] of page_table (int32, [sequences, pages]).  A packed
+    stream of prompts brings its position ids and Segments.seg_id.  Rows are quantised if the cache is int8 or float8_e4m3fn.
+    Tokens without a place (no such sequence, position or page) are left out.  Enqueues one kernel."""
+    _check("va_cache_write", lib().va_cache_write(k.data_ptr(), v.data_ptr(),
+                                                  *_cache_rows(k, v, cache, page_table, position_ids, seq_ids), _stream()))
+
+
+def paged_cache_read(cache, page_table: torch.Tensor, position_ids: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
+                     dtype: Optional[torch.dtype] = None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """-> K, V [N, Hkv, d]: the cached rows of the tokens that position_ids and seq_ids name as in paged_cache_write, zeros where there
+    is none.  dtype: of the rows out of an 8-bit cache (default bfloat16).  out: the two tensors to fill.  Enqueues one kernel."""
+    pages = cache[0]
+    if out is None:
+        dtype = dtype or (torch.bfloat16 if _CACHE_FORMATS.get(pages.dtype) else pages.dtype)
+        k, v = (torch.empty((position_ids.numel(), pages.shape[1], pages.shape[-1]), dtype=dtype, device=pages.device) for _ in "kv")
+    else:
+        k, v = out
+        if dtype is not None and k.dtype != dtype:
+            raise TypeError(f"out must hold {dtype}")
+    _check("va_cache_read", lib().va_cache_read(k.data_ptr(), v.data_ptr(),
+                                                *_cache_rows(k, v, cache, page_table, position_ids, seq_ids), _stream()))
+    return k, v
+
+
+def paged_attn_fwd(q: torch.Tensor, cache, page_table: torch.Tensor, context_lens: torch.Tensor, softmax_scale: float = 0.0, out=None,
+                   lse=None, workspace=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """One token of every sequence against its cached keys and values: q [B, Hq, d], page_table int32 [B, pages], context_lens int32
+    [B] (cached tokens, the new one's own included) -> O [B, Hq, d] (dtype of q), LSE [Hq, B] float32.  An empty sequence gives zeros
+    and -inf.  workspace: float32, of paged_attn_workspace(...)'s size, one for each of several calls that may overlap."""
+    c = _kv_cache(cache, page_table, q.dtype, q, context_lens)
+    if q.dim() != 3 or q.shape[2] != c.d or q.shape[0] != c.n_seqs or q.shape[1] % max(c.hkv, 1) or context_lens.shape != (c.n_seqs,):
+        raise ValueError(f"expected Q [{c.n_seqs}, a multiple of {c.hkv}, {c.d}] and {c.n_seqs} context lengths")
+    if context_lens.dtype != torch.int32:
+        raise TypeError("context_lens must be int32")
+    B, hq, d = q.shape
+    o = torch.empty_like(q) if out is None else _out_like("out", out, q.shape, q.dtype, q.device)
+    lse = (torch.empty((hq, B), dtype=torch.float32, device=q.device) if lse is None
+           else _out_like("lse", lse, (hq, B), torch.float32, q.device))
+    need = lib().va_paged_attn_workspace_bytes(B, c.max_pages, c.page_size, hq, c.hkv, d)
+    if workspace is None:
+        ws = torch.empty(need // 4, dtype=torch.float32, device=q.device)
+    else:
+        ws = workspace
+        _need_cuda(ws)
+        if ws.dtype != torch.float32 or ws.numel() * 4 < need or ws.device != q.device:
+            raise ValueError(f"workspace must be a contiguous float32 tensor of at least {need} bytes on {q.device}")
+    _check("va_paged_attn_fwd", lib().va_paged_attn_fwd(
+        q.data_ptr(), o.data_ptr(), lse.data_ptr(), _dt(q), C.byref(c), hq, context_lens.data_ptr(), float(softmax_scale),
+        ws.data_ptr(), ws.numel() * 4, _stream()))
+    return o, lse
+
+
+def paged_attn_workspace(q: torch.Tensor, cache, page_table: torch.Tensor) -> torch.Tensor:
+    """A workspace for paged_attn_fwd calls of these shapes."""
+    B, hq, d = q.shape
+    need = lib().va_paged_attn_workspace_bytes(B, page_table.shape[1], cache[0].shape[2], hq, cache[0].shape[1], d)
+    return torch.empty(need // 4, dtype=torch.float32, device=q.device)

@@ -271,6 +271,73 @@ va_status va_varlen_attn_bwd_noalloc(const void *dO, const void *Q, const void *
                             softmax_scale, ws, va_attn_workspace_bytes(rows * tokens_per_row, hq, hkv, d, 1), stream);
 }
 
+// ---- key-value cache ------------------------------------------------------------------------
+
+namespace {
+va_status check_cache(const va_kv_cache *c, va_dtype dt) {
+  if (!c) return VA_ERR_NULL;
+  if (c->n_pages <= 0 || c->page_size <= 0 || c->hkv <= 0 || c->d <= 0 || c->n_seqs < 0 || c->max_pages < 0) return VA_ERR_SHAPE;
+  if (c->table_stride < 0 || (c->n_seqs > 1 && c->table_stride < c->max_pages)) return VA_ERR_SHAPE;
+  constexpr long long kMost = 1ll << 31;
+  // three factors below 2^31: the first two fit in 64 bits, and are below 2^31 where the third is multiplied
+  const long long heads = (long long)c->n_pages * c->hkv;
+  if (heads >= kMost || heads * c->page_size >= kMost || (long long)c->max_pages * c->page_size >= kMost) return VA_ERR_SHAPE;
+  if ((long long)c->page_size * c->d >= 1ll << 26) return VA_ERR_SHAPE;
+  if (dt != VA_F32 && dt != VA_BF16 && dt != VA_F16) return VA_ERR_UNSUPPORTED;
+  if (c->format != VA_CACHE_PLAIN && c->format != VA_CACHE_I8 && c->format != VA_CACHE_E4M3) return VA_ERR_UNSUPPORTED;
+  if (c->d > 256 || c->hkv > 65535 || c->n_seqs > 65535) return VA_ERR_UNSUPPORTED;
+  if (!c->k || !c->v || (c->format != VA_CACHE_PLAIN && (!c->k_scale || !c->v_scale))) return VA_ERR_NULL;
+  if (!c->page_table && c->n_seqs > 0 && c->max_pages > 0) return VA_ERR_NULL;
+  return VA_OK;
+}
+}  // namespace
+
+va_status va_cache_write(const void *K, const void *V, va_dtype dt, const va_kv_cache *cache, const int32_t *seq_ids,
+                         const void *position_ids, va_itype it, int32_t n_tokens, void *stream) {
+  const va_status s = check_cache(cache, dt);
+  if (s != VA_OK) return s;
+  if (n_tokens < 0) return VA_ERR_SHAPE;
+  if (it != VA_I32 && it != VA_I64) return VA_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return VA_OK;
+  if (!K || !V || !position_ids) return VA_ERR_NULL;
+  return va::launch_cache_write(K, V, dt, *cache, seq_ids, position_ids, it, n_tokens, (hipStream_t)stream) == hipSuccess
+             ? VA_OK : VA_ERR_HIP;
+}
+
+va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache, const int32_t *seq_ids,
+                        const void *position_ids, va_itype it, int32_t n_tokens, void *stream) {
+  const va_status s = check_cache(cache, dt);
+  if (s != VA_OK) return s;
+  if (n_tokens < 0) return VA_ERR_SHAPE;
+  if (it != VA_I32 && it != VA_I64) return VA_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return VA_OK;
+  if (!K || !V || !position_ids) return VA_ERR_NULL;
+  return va::launch_cache_read(K, V, dt, *cache, seq_ids, position_ids, it, n_tokens, (hipStream_t)stream) == hipSuccess
+             ? VA_OK : VA_ERR_HIP;
+}
+
+size_t va_paged_attn_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t page_size, int32_t hq, int32_t hkv, int32_t d) {
+  if (n_seqs <= 0 || max_pages <= 0 || page_size <= 0 || hq <= 0 || hkv <= 0 || d <= 0) return 0;
+  return align_up(va::paged_workspace_bytes(n_seqs, (long long)max_pages * page_size, hq, hkv, d));
+}
+
+va_status va_paged_attn_fwd(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache *cache, int32_t hq,
+                            const int32_t *context_lens, float softmax_scale, void *workspace, size_t workspace_bytes,
+                            void *stream) {
+  const va_status s = check_cache(cache, dt);
+  if (s != VA_OK) return s;
+  if (hq <= 0 || hq % cache->hkv != 0) return VA_ERR_SHAPE;
+  if (hq > 65535) return VA_ERR_UNSUPPORTED;
+  if (cache->n_seqs == 0) return VA_OK;
+  if (!Q || !O || !LSE || !context_lens) return VA_ERR_NULL;
+  const size_t need = va_paged_attn_workspace_bytes(cache->n_seqs, cache->max_pages, cache->page_size, hq, cache->hkv, cache->d);
+  if (need > 0 && !workspace) return VA_ERR_NULL;
+  if (need > workspace_bytes || ((uintptr_t)workspace & 15) != 0) return VA_ERR_WORKSPACE;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->d);
+  return va::launch_paged(Q, O, LSE, dt, *cache, hq, context_lens, scale, (float *)workspace, (hipStream_t)stream) == hipSuccess
+             ? VA_OK : VA_ERR_HIP;
+}
+
 const char *va_status_string(va_status s) {
   switch (s) {
     case VA_OK: return "ok";

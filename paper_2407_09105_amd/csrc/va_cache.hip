@@ -1,0 +1,212 @@
+// Rows of K and V into the pages of the key-value cache, quantised on the way where the cache holds 8 bits, and back out of them
+// as a packed stream.
+//
+// Quantising a row x of d elements (one token and head): a = max |x_c|, scale = a / m, q_c = round(m x_c / a) with ties to even,
+// m = 127 (integers) or 448 (e4m3).  With a = 2^e f, f in [1/2, 1): q_c = round((x_c 2^-e m) / f), where the product is exact
+// for 16-bit x (8 or 11 bits times 7 or 3).  The quotient is product * RN(1 / f) corrected once by its remainder, two fused
+// multiply-adds: a quotient halfway between two steps comes out exactly, since its remainder is exact, and any other one of
+// 16-bit operands lies at least 2^-19 of itself away from halfway (the product has 18 bits at most), farther than the fp32
+// quotient is off.  So 16-bit rows are rounded exactly as real numbers would be, without a division per element.
+//
+// Bound by memory: each element is read once and written once.
+#include "va_kv_cache.h"
+
+namespace va {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) {
+  return it == VA_I64 ? (long long)((const int64_t *)ids)[t] : (long long)((const int32_t *)ids)[t];
+}
+
+// kLanes lanes hold a row, lane l its elements l * kVec .. + kVec - 1 (kStep = 1) or l, l + kLanes, ... (kVec = 1).
+template <class E, class C, int kVec, int kLanes>
+struct Row {
+  typedef typename E::elem elem;
+  typedef typename C::elem cached;
+  static constexpr int kPer = kVec > 1 ? kVec : 256 / kLanes;   // elements of a lane
+  static __device__ __forceinline__ int column(int lane, int e) { return kVec > 1 ? lane * kVec + e : lane + e * kLanes; }
+
+  template <class T> static __device__ __forceinline__ void load(const T *p, int lane, int d, T (&x)[kPer]) {
+    if constexpr (kVec > 1) {
+      struct __attribute__((aligned(sizeof(T) * kVec))) Chunk { T x[kVec]; };
+      if (lane * kVec < d) {
+        const Chunk c = *(const Chunk *)(p + lane * kVec);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) x[e] = c.x[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) x[e] = (T)0;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[e] = column(lane, e) < d ? p[column(lane, e)] : (T)0;
+    }
+  }
+  template <class T> static __device__ __forceinline__ void store(T *p, int lane, int d, const T (&x)[kPer]) {
+    if constexpr (kVec > 1) {
+      struct __attribute__((aligned(sizeof(T) * kVec))) Chunk { T x[kVec]; };
+      if (lane * kVec < d) {
+        Chunk c;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) c.x[e] = x[e];
+        *(Chunk *)(p + lane * kVec) = c;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (column(lane, e) < d) p[column(lane, e)] = x[e];
+    }
+  }
+
+  static __device__ __forceinline__ int8_t rounded(I8, float t) { return (int8_t)(int)rintf(t); }
+  static __device__ __forceinline__ uint8_t rounded(E4m3, float t) { return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(t, t, 0, false); }
+
+  // The row in 8 bits; returns its scale, the same in all of its lanes.
+  static __device__ __forceinline__ float quantise(const elem (&x)[kPer], cached (&q)[kPer]) {
+    uint32_t top = 0;  // magnitudes compare as their bits do; a NaN is above infinity
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) top = max(top, __float_as_uint((float)x[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o, kLanes));
+    const bool finite = top < 0x7f800000u;
+    const float a = finite ? __uint_as_float(top) : 0.f;
+    int ex = 0;
+    float f = frexpf(a, &ex);
+    if (ex < -100) f = ldexpf(f, ex + 100), ex = -100;  // m 2^-e stays in range; f > 2^-50
+    const float pre = ldexpf(C::kTop, -ex), inv = a > 0.f ? 1.f / f : 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const float n = finite ? (float)x[e] * pre : 0.f, t = n * inv;
+      q[e] = (cached)rounded(C(), fmaf(fmaf(-t, f, n), inv, t));
+    }
+    return finite ? fminf(a / C::kTop, C::kMostScale) : __uint_as_float(0x7fc00000u);
+  }
+};
+
+// One row of K and of V per kLanes lanes; workgroup: kThreads / kLanes consecutive tokens of one head.
+template <class E, class C, int kVec, int kLanes>
+__global__ void __launch_bounds__(kThreads)
+write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
+             typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, int H, int d) {
+  typedef Row<E, C, kVec, kLanes> R;
+  const int lane = threadIdx.x % kLanes, g = blockIdx.x % H;
+  const long long t = (long long)(blockIdx.x / H) * (kThreads / kLanes) + threadIdx.x / kLanes;
+  if (t >= N) return;
+  const int place = place_of(map, seq_ids ? seq_ids[t] : t, id_at(pos, it, (int)t));
+  if (place < 0) return;
+  const size_t row = (size_t)place + (size_t)g * map.page.d, from = ((size_t)t * H + g) * d;
+  typename E::elem k[R::kPer], v[R::kPer];
+  R::load(K + from, lane, d, k);
+  R::load(V + from, lane, d, v);
+  if constexpr (is_8bit<C>::value) {
+    typename C::elem q[R::kPer];
+    const float sk = R::quantise(k, q);
+    R::store(Kc + row * d, lane, d, q);
+    const float sv = R::quantise(v, q);
+    R::store(Vc + row * d, lane, d, q);
+    if (lane == 0) {
+      ks[row] = sk;
+      vs[row] = sv;
+    }
+  } else {
+    R::store(Kc + row * d, lane, d, k);
+    R::store(Vc + row * d, lane, d, v);
+  }
+}
+
+template <class E, class C, int kVec, int kLanes>
+__global__ void __launch_bounds__(kThreads)
+read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
+            const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, int H, int d) {
+  typedef Row<E, C, kVec, kLanes> R;
+  const int lane = threadIdx.x % kLanes, g = blockIdx.x % H;
+  const long long t = (long long)(blockIdx.x / H) * (kThreads / kLanes) + threadIdx.x / kLanes;
+  if (t >= N) return;
+  const int place = place_of(map, seq_ids ? seq_ids[t] : t, id_at(pos, it, (int)t));
+  const size_t row = (size_t)place + (size_t)g * map.page.d, to = ((size_t)t * H + g) * d;
+  typename E::elem k[R::kPer] = {}, v[R::kPer] = {};
+  if (place >= 0) {
+    if constexpr (is_8bit<C>::value) {
+      typename C::elem qk[R::kPer], qv[R::kPer];
+      R::load(Kc + row * d, lane, d, qk);
+      R::load(Vc + row * d, lane, d, qv);
+      const float sk = ks[row], sv = vs[row];
+#pragma unroll
+      for (int e = 0; e < R::kPer; ++e) {
+        k[e] = (typename E::elem)(cached_to_f32(C(), qk[e]) * sk);
+        v[e] = (typename E::elem)(cached_to_f32(C(), qv[e]) * sv);
+      }
+    } else {
+      R::load(Kc + row * d, lane, d, k);
+      R::load(Vc + row * d, lane, d, v);
+    }
+  }
+  R::store(K + to, lane, d, k);
+  R::store(V + to, lane, d, v);
+}
+
+struct Call {
+  const void *K, *V;  // written to by a read
+  const va_kv_cache &c;
+  const int32_t *seq_ids;
+  const void *pos;
+  va_itype it;
+  int N;
+  bool write;
+  hipStream_t stream;
+};
+
+template <class E, class C, int kVec, int kLanes> hipError_t launch(const Call &a) {
+  typedef typename E::elem elem;
+  typedef typename C::elem cached;
+  constexpr int kTokens = kThreads / kLanes;
+  const long long groups = ((long long)a.N + kTokens - 1) / kTokens * a.c.hkv;
+  if (groups > 0x7fffffffll) return hipErrorInvalidValue;
+  const PageMap map = page_map(a.c);
+  if (a.write)
+    write_kernel<E, C, kVec, kLanes><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+        (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+        a.N, a.c.hkv, a.c.d);
+  else
+    read_kernel<E, C, kVec, kLanes><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+        (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+        a.N, a.c.hkv, a.c.d);
+  return hipGetLastError();
+}
+
+// Chunks of 16 bytes of K and V where the rows of both sides consist of whole aligned ones, else single elements.
+template <class E, class C> hipError_t launch_ec(const Call &a) {
+  constexpr int kVec = 16 / sizeof(typename E::elem);
+  const uintptr_t cached_at = (uintptr_t)a.c.k | (uintptr_t)a.c.v, rows_at = (uintptr_t)a.K | (uintptr_t)a.V;
+  if (a.c.d % kVec != 0 || rows_at % 16 != 0 || cached_at % (kVec * sizeof(typename C::elem)) != 0) return launch<E, C, 1, 64>(a);
+  const int chunks = a.c.d / kVec;
+  if (chunks <= 8) return launch<E, C, kVec, 8>(a);
+  if (chunks <= 16) return launch<E, C, kVec, 16>(a);
+  if (chunks <= 32) return launch<E, C, kVec, 32>(a);
+  return launch<E, C, kVec, 64>(a);
+}
+template <class E> hipError_t launch_e(const Call &a) {
+  if (a.c.format == VA_CACHE_I8) return launch_ec<E, I8>(a);
+  if (a.c.format == VA_CACHE_E4M3) return launch_ec<E, E4m3>(a);
+  return launch_ec<E, E>(a);
+}
+hipError_t launch_dt(va_dtype dt, const Call &a) {
+  return dt == VA_BF16 ? launch_e<Bf16>(a) : dt == VA_F16 ? launch_e<F16>(a) : launch_e<F32>(a);
+}
+
+}  // namespace
+
+hipError_t launch_cache_write(const void *K, const void *V, va_dtype dt, const va_kv_cache &cache, const int32_t *seq_ids,
+                              const void *pos, va_itype it, int N, hipStream_t stream) {
+  return launch_dt(dt, {K, V, cache, seq_ids, pos, it, N, true, stream});
+}
+hipError_t launch_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache &cache, const int32_t *seq_ids, const void *pos,
+                             va_itype it, int N, hipStream_t stream) {
+  return launch_dt(dt, {K, V, cache, seq_ids, pos, it, N, false, stream});
+}
+
+}  // namespace va

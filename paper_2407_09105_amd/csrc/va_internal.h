@@ -60,4 +60,15 @@ hipError_t launch_mfma_bwd(const void *dO, const void *Q, const void *K, const v
                            int hkv, int d, va_dtype dt, float scale, const Partials &partial, hipStream_t stream,
                            unsigned stages);
 
+// va_cache.hip: rows into and out of the key-value cache
+hipError_t launch_cache_write(const void *K, const void *V, va_dtype dt, const va_kv_cache &cache, const int32_t *seq_ids,
+                              const void *pos, va_itype it, int N, hipStream_t stream);
+hipError_t launch_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache &cache, const int32_t *seq_ids, const void *pos,
+                             va_itype it, int N, hipStream_t stream);
+
+// va_paged.hip: attention of one token per sequence over the key-value cache
+size_t paged_workspace_bytes(int n_seqs, long long capacity, int hq, int hkv, int d);
+hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache &cache, int hq, const int32_t *lens,
+                        float scale, float *workspace, hipStream_t stream);
+
 }  // namespace va
