@@ -247,7 +247,8 @@ va_status va_varlen_attn_bwd_stages(const void *dO, const void *Q, const void *K
  *   page_table       : device, [n_seqs] rows of max_pages int32, table_stride entries apart: position p of sequence s lies in
  *                      page page_table[s * table_stride + p / page_size], at place p % page_size.  An entry outside
  *                      [0, n_pages) is no page; sequences may share pages.
- * Limits: n_pages * hkv * page_size < 2^31 (rows of one tensor), max_pages * page_size < 2^31, page_size * d < 2^26, n_seqs <= 65535.
+ * Limits: n_pages * hkv * page_size < 2^31 (rows of one tensor), max_pages * page_size <= 2^31 - 2^10,
+ * page_size * d < 2^26, n_seqs <= 65535.
  */
 typedef enum {
   VA_CACHE_PLAIN = 0, /* elements of the type that the call names for K and V (or Q)            */

@@ -281,7 +281,7 @@ va_status check_cache(const va_kv_cache *c, va_dtype dt) {
   constexpr long long kMost = 1ll << 31;
   // three factors below 2^31: the first two fit in 64 bits, and are below 2^31 where the third is multiplied
   const long long heads = (long long)c->n_pages * c->hkv;
-  if (heads >= kMost || heads * c->page_size >= kMost || (long long)c->max_pages * c->page_size >= kMost) return VA_ERR_SHAPE;
+  if (heads >= kMost || heads * c->page_size >= kMost || (long long)c->max_pages * c->page_size > kMost - 1024) return VA_ERR_SHAPE;
   if ((long long)c->page_size * c->d >= 1ll << 26) return VA_ERR_SHAPE;
   if (dt != VA_F32 && dt != VA_BF16 && dt != VA_F16) return VA_ERR_UNSUPPORTED;
   if (c->format != VA_CACHE_PLAIN && c->format != VA_CACHE_I8 && c->format != VA_CACHE_E4M3) return VA_ERR_UNSUPPORTED;

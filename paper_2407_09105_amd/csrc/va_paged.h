@@ -1,0 +1,630 @@
+// Attention of one new token of every sequence over the paged key-value cache: the kernel (instantiated in va_paged_*.hip, one
+// file per type of the queries) and what it shares with the joining of parts (va_paged.hip).
+//
+// A wave takes 32 keys at a time for the (up to 16) query heads of a KV head, straight from memory into registers: no LDS, no
+// barrier, until the waves' results are joined at the end.  With v_mfma_f32_16x16x32 (lane l: i = l % 16, h = l / 16; operand
+// A row i, B column i, both at k = 8 h + 0..7; result: column i, rows 4 h + 0..3):
+//   - S^T = K Q^T, two products of 16 keys: lane (i, h) loads 16-byte chunks h, h + 4, ... of key i's row - which columns share a
+//     k-step does not matter as long as q's fragments hold the same ones - and ends up with scores of head i, keys 4 h + 0..3.
+//   - O^T += V^T P^T: those 2 x 4 keys are k = 8 h + 0..7, so P^T needs no exchange between lanes.  Lane (i, h) loads columns
+//     8 i + 0..7 of its 8 keys (16 lanes together a whole row of 128 columns); the fragment of the m-th product, whose rows are the
+//     columns 8 i + m, is the m-th element of each of them: four byte permutations, half an instruction per element.
+// Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  P enters the
+// matrix unit in two 16-bit parts (the second holds what the first cuts off, 2^-15 of P remain): the matrix unit is idle nine
+// tenths of the time, and the result is as exact as fp32 probabilities make it.
+//
+// Bound by memory: keys and values are read once, 2 d bytes each against 4 d flops per query head.
+#pragma once
+#include "va_kv_cache.h"
+
+namespace va {
+namespace paged {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kTile = 32;               // keys of a wave's step
+constexpr int kUnit = kTile * kWaves;   // sequences are cut at multiples of this
+constexpr int kHeads = 16;              // query heads of a workgroup
+constexpr float kLazyLog2 = 8.f;
+
+// How the sequences are cut into parts, one workgroup's work per KV head: see find_part.
+struct Split {
+  int slots;        // room for parts; n_seqs where no sequence is cut
+  int least_units;  // least length of a part
+};
+Split split_of(int n_seqs, long long capacity, int hq, int hkv);
+
+// Parts of all sequences in order: [slots, hq, d] sums of P V, then [slots, hq] pairs (reference exponent, sum of P).
+struct Workspace {
+  float *o;
+  float2 *ml;
+};
+static inline Workspace workspace(float *p, const Split &s, int hq, int d) {
+  const size_t n = (size_t)s.slots * hq * d;
+  return {p, (float2 *)(p + (n + 1) / 2 * 2)};
+}
+
+struct Part {
+  int b, first, parts;  // sequence, its first part's slot, how many it has
+  int units;            // of kUnit keys in a part
+  int n;                // tokens of the sequence
+};
+
+// The part that a slot holds, false where it holds none; with slot < 0 the first part of sequence seq.  A sequence of u units has max(1, ceil(u / c)) parts of c units, where
+// c = max(least_units, ceil(all units / (slots - n_seqs))): no more than slots in all, whatever the lengths are, and of equal
+// size but for the last of each sequence.  A wave reads 64 lengths at a time and adds them up across its lanes.
+__device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, const PageMap &map, const Split &split, int slot, int seq,
+                                          Part &part) {
+  const int lane = threadIdx.x & 63, B = map.n_seqs;
+  auto length = [&](int b) { return b < B ? min(max(lens[b], 0), map.capacity) : 0; };
+  if (split.slots == B) {
+    seq = slot < 0 ? seq : slot;
+    part = {seq, seq, 1, 0x7fffffff / kUnit, uniform(length(seq))};
+    return true;
+  }
+  double total = 0;  // exact: below 2^53
+  int mine = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    mine = length(b0 + lane);
+    total += (double)((mine + kUnit - 1) / kUnit);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
+  const int c = uniform(max(split.least_units, (int)fmin(ceil(total / (split.slots - B)), 0x7fffffff / kUnit)));
+  int before = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    if (B > 64) mine = length(b0 + lane);
+    const int units = (mine + kUnit - 1) / kUnit;
+    const int parts = b0 + lane < B ? max(1, (units + c - 1) / c) : 0;
+    int upto = parts;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t past = slot < 0 ? __ballot(b0 + lane >= seq) : __ballot(before + upto > slot);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      part = {b0 + at, before + __builtin_amdgcn_readlane(upto - parts, at), __builtin_amdgcn_readlane(parts, at), c,
+              __builtin_amdgcn_readlane(mine, at)};
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// max / sum over the four lanes that hold a head
+__device__ __forceinline__ float head_max(float x) {
+  x = pair_max(x);
+  return fmaxf(x, __shfl_xor(x, 16));
+}
+__device__ __forceinline__ float head_sum(float x) {
+  x = pair_sum(x);
+  return x + __shfl_xor(x, 16);
+}
+
+// ---- element types ----------------------------------------------------------------------------------
+
+template <class E> struct is_f32 { static constexpr bool value = false; };
+template <> struct is_f32<F32> { static constexpr bool value = true; };
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Four cached 8-bit elements (one dword) as 16-bit elements of E, two dwords, or as floats; all exact.
+__device__ __forceinline__ void widen(E4m3, Bf16, uint32_t x, uint32_t (&y)[2]) {
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true));
+}
+__device__ __forceinline__ void widen(E4m3, F16, uint32_t x, uint32_t (&y)[2]) {
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false));
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true));
+}
+__device__ __forceinline__ void floats(I8, uint32_t x, float (&y)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(x >> (8 * e));
+}
+__device__ __forceinline__ void floats(E4m3, uint32_t x, float (&y)[4]) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+  y[0] = a[0], y[1] = a[1], y[2] = b[0], y[3] = b[1];
+}
+__device__ __forceinline__ void widen(I8, Bf16, uint32_t x, uint32_t (&y)[2]) {
+  float f[4];
+  floats(I8(), x, f);  // eight significant bits at most: the upper halves hold them
+  y[0] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+  y[1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+}
+__device__ __forceinline__ void widen(I8, F16, uint32_t x, uint32_t (&y)[2]) {
+  // the bytes 128 higher, behind the exponent of 1024: 1024 + 128 + x, exactly
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+  x ^= 0x80808080u;
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u)) - off);
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u)) - off);
+}
+
+// P (>= 0) in two parts of 16 bits.  The first is cut off, not rounded, and the second holds the rest and 2^-20 more: positive like
+// P, so that an infinity in V comes out as one.
+__device__ __forceinline__ void two_parts(Bf16, const float (&p)[8], bf16x8 &hi, bf16x8 &lo) {
+  u32x4 h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) lo[e] = (__bf16)fmaf(p[e], 0x1p-20f, p[e] - __uint_as_float(__float_as_uint(p[e]) & 0xffff0000u));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
+  hi = as_x8<Bf16>(h);
+}
+__device__ __forceinline__ void two_parts(F16, const float (&p)[8], f16x8 &hi, f16x8 &lo) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const auto h = __builtin_amdgcn_cvt_pkrtz(p[e], p[e + 1]);
+    hi[e] = (_Float16)h[0], hi[e + 1] = (_Float16)h[1];
+    lo[e] = (_Float16)fmaf(p[e], 0x1p-20f, p[e] - (float)h[0]);
+    lo[e + 1] = (_Float16)fmaf(p[e + 1], 0x1p-20f, p[e + 1] - (float)h[1]);
+  }
+}
+// P is kept this many powers of two above exp(S - maximum): fp16 has few exponents below 1.
+template <class E> struct shift_log2 { static constexpr float value = 0.f; };
+template <> struct shift_log2<F16> { static constexpr float value = 6.f; };
+
+// ---- the kernel ---------------------------------------------------------------------------------------
+
+// How a tile's rows are found: kInPage: page_size is a multiple of 16, and the 16 keys of a product lie next to each other; kPerKey:
+// each key on its own; kElements: likewise, and rows are read element by element (head dims or addresses that 16-byte chunks do not
+// fit).
+enum Look { kInPage, kPerKey, kElements };
+
+struct Args {
+  const void *Q;
+  void *O;
+  float *LSE;
+  const void *k, *v;
+  const float *ks, *vs;
+  PageMap map;
+  const int32_t *lens;
+  Split split;
+  Workspace ws;
+  int hq, d;
+  float scale_log2;
+};
+
+template <int kBytes> struct Piece {
+  uint32_t x[kBytes / 4];
+};
+template <int kBytes> __device__ __forceinline__ Piece<kBytes> buffer_piece(buffer_t b, uint32_t off) {
+  Piece<kBytes> p;
+  if constexpr (kBytes == 16) {
+    const u32x4 r = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.x[i] = r[i];
+  } else if constexpr (kBytes == 8) {
+    const u32x2 r = __builtin_amdgcn_raw_buffer_load_b64(b, (int)off, 0, 0);
+    p.x[0] = r[0], p.x[1] = r[1];
+  } else {
+    p.x[0] = __builtin_amdgcn_raw_buffer_load_b32(b, (int)off, 0, 0);
+  }
+  return p;
+}
+template <int kBytes> __device__ __forceinline__ Piece<kBytes> memory_piece(const char *p) {
+  struct __attribute__((packed, aligned(4))) Raw { uint32_t x[kBytes / 4]; };
+  const Raw r = *(const Raw *)p;
+  Piece<kBytes> q;
+#pragma unroll
+  for (int i = 0; i < kBytes / 4; ++i) q.x[i] = r.x[i];
+  return q;
+}
+// elements `column` .. of a row of d elements, zeros behind it
+template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_piece(const T *row, int column, int d) {
+  constexpr int kEach = 4 / sizeof(T);
+  Piece<kBytes> p;
+#pragma unroll
+  for (int i = 0; i < kBytes / 4; ++i) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int c = column + i * kEach + e;
+      uint32_t bits = 0;
+      if (c < d) {
+        if constexpr (sizeof(T) == 1) bits = *(const uint8_t *)(row + c);
+        else if constexpr (sizeof(T) == 2) bits = *(const uint16_t *)(row + c);
+        else bits = *(const uint32_t *)(row + c);
+      }
+      w |= bits << (8 * sizeof(T) * e % 32);
+    }
+    p.x[i] = w;
+  }
+  return p;
+}
+
+// E: type of the queries; C: of the cache (E itself or 8 bits); kDh: head_dim rounded up to 64, 128 or 256.
+template <class E, class C, int kDh, Look kLook>
+__global__ void __launch_bounds__(kThreads, is_f32<E>::value ? (kDh == 256 ? 1 : 2) : kDh == 256 ? 2 : 3)
+kernel(Args a) {
+  constexpr bool kF32 = is_f32<E>::value, k8 = is_8bit<C>::value;
+  typedef typename E::elem elem;
+  typedef typename C::elem cached;
+  constexpr int kSize = sizeof(cached);
+  // K: chunks of 16 bytes, chunk n of lane (i, h) = columns (4 n + h) kCpc ..
+  constexpr int kCpc = 16 / kSize, kKn = kDh / (4 * kCpc);
+  // V: kVC columns of a row for a lane at a time, kHf times
+  constexpr int kVC = kF32 || kDh == 64 ? 4 : 8, kHf = kDh / (16 * kVC), kVBytes = kVC * kSize;
+  // matrix operands: of the queries' type, but P goes with 8-bit values as bf16, which has the range for their scales
+  typedef typename std::conditional<kF32, Bf16, E>::type E16;
+  typedef typename std::conditional<k8, Bf16, E16>::type P16;
+  typedef typename E16::x8 qx8;
+  typedef typename P16::x8 px8;
+  constexpr float kShift = kF32 ? 0.f : shift_log2<P16>::value;
+
+  constexpr int kStride = 16 * kVC + 4;
+  __shared__ __attribute__((aligned(16))) float part_o[kWaves][kHeads][kStride];
+  __shared__ float part_m[kWaves][kHeads], part_l[kWaves][kHeads];
+
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), i = lane & 15, h = lane >> 4;
+  const PageMap &map = a.map;
+  const int hkv = map.hkv, d = a.d, G = a.hq / hkv, page = map.page.d;
+
+  // Workgroup ids go to the 8 XCDs in turn: the groups of 16 query heads of one KV head, which read the same keys, 8 ids apart.
+  const int groups = (G + kHeads - 1) / kHeads, turn = blockIdx.x >> 3;
+  const int pair = turn / groups * 8 + (blockIdx.x & 7), head0 = turn % groups * kHeads;
+  if (pair >= a.split.slots * hkv) return;
+  const int slot = pair / hkv, g = pair - slot * hkv;
+  Part part;
+  if (!find_part(a.lens, map, a.split, slot, 0, part)) return;
+  const int b = part.b, n = part.n;
+  const int heads = min(G - head0, kHeads);  // rows of this workgroup
+  const size_t first_head = (size_t)b * a.hq + g * G + head0;
+
+  // q as operand B: head i, the columns of the K chunks
+  constexpr int kQf = kF32 ? kKn * kCpc : kKn * kCpc / 8;
+  typename std::conditional<kF32, float, qx8>::type qf[kQf];
+  {
+    const elem *q = (const elem *)a.Q + (first_head + min(i, heads - 1)) * d;
+    auto q_at = [&](int column) { return i < heads && column < d ? q[min(column, d - 1)] : (elem)0.f; };
+#pragma unroll
+    for (int x = 0; x < kKn; ++x)
+#pragma unroll
+      for (int e = 0; e < kCpc; ++e) {
+        const elem y = q_at((4 * x + h) * kCpc + e);
+        if constexpr (kF32) qf[x * kCpc + e] = y;
+        else qf[(x * kCpc + e) / 8][e % 8] = y;
+      }
+  }
+
+  // keys j0 .. j1 - 1, tiles wave, wave + kWaves, ...
+  const long long j0l = (long long)(slot - part.first) * part.units * kUnit;
+  const int j0 = (int)min(j0l, (long long)n), j1 = (int)min(j0l + (long long)part.units * kUnit, (long long)n);
+  const int tile_end = (j1 + kTile - 1) / kTile;
+  const int32_t *const table = map.table + (int64_t)b * map.stride;
+
+  // ---- rows of a tile ----
+  struct Rows {
+    int row[2];    // kInPage: row of the product's first key; else of this lane's key i; its scales
+    int count[2];  // kInPage: keys that exist; else 1 or 0 for key i
+  };
+  auto find_rows = [&](int tile) {
+    Rows r;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int j = tile * kTile + 16 * s + (kLook == kInPage ? 0 : i);
+      int at = 0, id = -1;
+      if ((uint32_t)j < (uint32_t)j1) at = j / map.page, id = table[at];
+      const bool ok = (uint32_t)id < (uint32_t)map.n_pages;
+      r.row[s] = ok ? (id * hkv + g) * page + (j - at * page) : 0;
+      r.count[s] = !ok ? 0 : kLook == kInPage ? min(j1 - j, 16) : 1;
+    }
+    return r;
+  };
+
+  const uint32_t row_bytes = (uint32_t)d * kSize;
+  uint32_t k_off[kKn], v_off[kHf];  // column offsets in a row, kPastEnd for columns that do not exist
+#pragma unroll
+  for (int x = 0; x < kKn; ++x) k_off[x] = (4 * x + h) * kCpc < d ? (uint32_t)(i * row_bytes + (4 * x + h) * 16) : kPastEnd;
+#pragma unroll
+  for (int x = 0; x < kHf; ++x) v_off[x] = (16 * x + i) * kVC < d ? (uint32_t)(4 * h * row_bytes + (16 * x + i) * kVBytes) : kPastEnd;
+  const bool half_chunk = k8 && (d & 8) != 0;  // rows end in the middle of a 16-byte chunk
+
+  typedef Piece<16> KPiece;
+  typedef Piece<kVBytes> VPiece;
+  KPiece kr[2][kKn];
+  VPiece vr[8][kHf];
+  f32x4 ksr[2], vsr[2];
+
+  auto load_k = [&](const Rows &r) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (kLook == kInPage) {
+        const buffer_t buf = make_buffer((const char *)a.k + (size_t)r.row[s] * row_bytes, (size_t)r.count[s] * row_bytes);
+        if (!half_chunk) {
+#pragma unroll
+          for (int x = 0; x < kKn; ++x) kr[s][x] = buffer_piece<16>(buf, k_off[x]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < kKn; ++x) {
+            const Piece<8> lo = buffer_piece<8>(buf, k_off[x]);
+            const Piece<8> hi = buffer_piece<8>(buf, (4 * x + h) * kCpc + 8 < d ? k_off[x] + 8 : kPastEnd);
+            kr[s][x] = {{lo.x[0], lo.x[1], hi.x[0], hi.x[1]}};
+          }
+        }
+        if constexpr (k8) {
+          const buffer_t sb = make_buffer(a.ks + r.row[s], r.count[s] > 0 ? 64 : 0);
+          const Piece<16> y = buffer_piece<16>(sb, 16 * h);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) ksr[s][v] = __uint_as_float(y.x[v]);
+        }
+      } else {
+        const char *row = (const char *)a.k + (size_t)r.row[s] * row_bytes;  // row 0 for a key that does not exist
+        if constexpr (kLook == kElements) {
+#pragma unroll
+          for (int x = 0; x < kKn; ++x) kr[s][x] = element_piece<cached, 16>((const cached *)row, (4 * x + h) * kCpc, d);
+        } else if (d == kDh) {
+#pragma unroll
+          for (int x = 0; x < kKn; ++x) kr[s][x] = memory_piece<16>(row + (4 * x + h) * 16);
+        } else {
+#pragma unroll
+          for (int x = 0; x < kKn; ++x) {
+            const int column = (4 * x + h) * kCpc;
+            kr[s][x] = {};
+            if (column + kCpc <= d) {
+              kr[s][x] = memory_piece<16>(row + column * kSize);
+            } else if (half_chunk && column < d) {
+              const Piece<8> lo = memory_piece<8>(row + column * kSize);
+              kr[s][x].x[0] = lo.x[0], kr[s][x].x[1] = lo.x[1];
+            }
+          }
+        }
+        if constexpr (k8) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) ksr[s][v] = a.ks[__shfl(r.row[s], 4 * h + v)];
+        }
+      }
+    }
+  };
+  auto load_v = [&](const Rows &r) {
+    const bool all = kLook == kPerKey && d == 16 * kVC * kHf && !__any(r.count[0] == 0 || r.count[1] == 0);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (kLook == kInPage) {
+        const buffer_t buf = make_buffer((const char *)a.v + (size_t)r.row[s] * row_bytes, (size_t)r.count[s] * row_bytes);
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = buffer_piece<kVBytes>(buf, v_off[x] == kPastEnd ? kPastEnd : v_off[x] + v * row_bytes);
+        if constexpr (k8) {
+          const buffer_t sb = make_buffer(a.vs + r.row[s], r.count[s] > 0 ? 64 : 0);
+          const Piece<16> y = buffer_piece<16>(sb, 16 * h);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) vsr[s][v] = __uint_as_float(y.x[v]);
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int from = __shfl(r.row[s], 4 * h + v);
+          const bool ok = __shfl(r.count[s], 4 * h + v) != 0;
+          const char *row = (const char *)a.v + (size_t)from * row_bytes;
+          if constexpr (kLook == kElements) {
+#pragma unroll
+            for (int x = 0; x < kHf; ++x)
+              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, ok ? d : 0);
+          } else if (all) {
+#pragma unroll
+            for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
+          } else {
+#pragma unroll
+            for (int x = 0; x < kHf; ++x) {
+              vr[4 * s + v][x] = {};
+              if (ok && (16 * x + i) * kVC < d) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
+            }
+          }
+          if constexpr (k8) vsr[s][v] = ok ? a.vs[from] : 0.f;
+        }
+      }
+    }
+  };
+
+  f32x4 acc[kHf][kVC];
+#pragma unroll
+  for (int x = 0; x < kHf; ++x)
+#pragma unroll
+    for (int m = 0; m < kVC; ++m) acc[x][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_ref = -INFINITY, m_thr = -INFINITY;  // raw score that exponents are relative to, and the one that moves it
+  float l_run = 0.f;                           // this lane's share of the sum of P
+
+  int tile = j0 / kTile + wave;
+  Rows now = find_rows(tile);
+  if (tile < tile_end) load_k(now);
+  for (; tile < tile_end; tile += kWaves) {
+    const Rows next = find_rows(tile + kWaves);  // no keys behind the last tile
+    load_v(now);
+    // ---- S^T = K Q^T ----
+    f32x4 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < kKn; ++x) {
+        const KPiece &p = kr[t][x];
+        if constexpr (kF32 && k8) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float f[4];
+            floats(C(), p.x[w], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t] = mfma16(f[e], qf[x * kCpc + 4 * w + e], s[t]);
+          }
+        } else if constexpr (kF32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t] = mfma16(__uint_as_float(p.x[e]), qf[x * kCpc + e], s[t]);
+        } else if constexpr (k8) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t w0[2], w1[2];
+            widen(C(), E16(), p.x[2 * y], w0);
+            widen(C(), E16(), p.x[2 * y + 1], w1);
+            s[t] = mfma16(as_x8<E16>(u32x4{w0[0], w0[1], w1[0], w1[1]}), qf[2 * x + y], s[t]);
+          }
+        } else {
+          s[t] = mfma16(as_x8<E16>(u32x4{p.x[0], p.x[1], p.x[2], p.x[3]}), qf[x], s[t]);
+        }
+      }
+      if constexpr (k8) s[t] *= ksr[t];
+    }
+    if (tile + kWaves < tile_end) load_k(next);
+    // ---- keys that do not exist ----
+    if constexpr (kLook == kInPage) {
+      if (now.count[0] + now.count[1] < kTile) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const bool there = 4 * h + v < now.count[t];
+            s[t][v] = there ? s[t][v] : -INFINITY;
+            if constexpr (k8) vsr[t][v] = there ? vsr[t][v] : 0.f;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t there = (uint32_t)__ballot(now.count[t] != 0) & 0xffffu;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[t][v] = there >> (4 * h + v) & 1 ? s[t][v] : -INFINITY;
+      }
+    }
+    // ---- softmax ----
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__any(mx > m_thr)) {
+      const float m_new = fmaxf(m_ref, head_max(mx));
+      const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_ref - m_new) * a.scale_log2);
+      l_run *= alpha;  // a NaN of before stays
+#pragma unroll
+      for (int x = 0; x < kHf; ++x)
+#pragma unroll
+        for (int m = 0; m < kVC; ++m) acc[x][m] *= alpha;
+      m_ref = m_new;
+      m_thr = m_new + kLazyLog2 / a.scale_log2;
+    }
+    const float base = m_ref == -INFINITY ? 0.f : m_ref;
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3] - base, a.scale_log2, kShift));
+      l_run += p[e];
+    }
+    if constexpr (k8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] *= vsr[e >> 2][e & 3];
+    }
+    // ---- O^T += V^T P^T ----
+    if constexpr (kF32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int x = 0; x < kHf; ++x) {
+          float f[4];
+          if constexpr (k8) floats(C(), vr[e][x].x[0], f);
+          else
+#pragma unroll
+            for (int m = 0; m < 4; ++m) f[m] = __uint_as_float(vr[e][x].x[m]);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) acc[x][m] = mfma16(f[m], p[e], acc[x][m]);
+        }
+    } else {
+      px8 hi, lo;
+      two_parts(P16(), p, hi, lo);
+#pragma unroll
+      for (int x = 0; x < kHf; ++x) {
+        uint32_t w[8][kVC / 2];  // columns in pairs
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (k8) {
+#pragma unroll
+            for (int y = 0; y < kVC / 4; ++y) {
+              uint32_t two[2];
+              widen(C(), P16(), vr[e][x].x[y], two);
+              w[e][2 * y] = two[0], w[e][2 * y + 1] = two[1];
+            }
+          } else {
+#pragma unroll
+            for (int y = 0; y < kVC / 2; ++y) w[e][y] = vr[e][x].x[y];
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < kVC; ++m) {
+          u32x4 f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = __builtin_amdgcn_perm(w[2 * e + 1][m / 2], w[2 * e][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
+          const px8 vf = as_x8<P16>(f);
+          acc[x][m] = mfma16(vf, lo, acc[x][m]);
+          acc[x][m] = mfma16(vf, hi, acc[x][m]);
+        }
+      }
+    }
+    now = next;
+  }
+
+  // ---- the waves' results: relative to the largest reference, added in order ----
+  l_run = head_sum(l_run);
+  if (h == 0) part_m[wave][i] = m_ref, part_l[wave][i] = l_run;
+#pragma unroll
+  for (int x = 0; x < kHf; ++x) {
+    if (x > 0) __syncthreads();  // the columns before are read
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+#pragma unroll
+      for (int m = 0; m < kVC; m += 4)
+        *(f32x4 *)&part_o[wave][i][kVC * (4 * h + v) + m] = f32x4{acc[x][m][v], acc[x][m + 1][v], acc[x][m + 2][v], acc[x][m + 3][v]};
+    __syncthreads();
+    for (int at = threadIdx.x; at < heads * 16 * kVC; at += kThreads) {
+      const int head = at / (16 * kVC), c = at % (16 * kVC), column = 16 * kVC * x + c;
+      if (column >= d) continue;
+      float m = part_m[0][head], sum = 0.f, o = 0.f;
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w][head]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = part_m[w][head], weight = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - m) * a.scale_log2);
+        sum += weight * part_l[w][head];
+        o += weight * part_o[w][head][c];
+      }
+      const float exponent = m * a.scale_log2 - kShift;
+      if (part.parts == 1) {
+        ((elem *)a.O)[(first_head + head) * d + column] = (elem)(sum != 0.f ? o / sum : 0.f);
+        if (column == 0)
+          a.LSE[(size_t)(g * G + head0 + head) * map.n_seqs + b] = sum != 0.f ? (exponent + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+      } else {
+        const size_t to = (size_t)slot * a.hq + g * G + head0 + head;
+        a.ws.o[to * d + column] = o;
+        if (column == 0) a.ws.ml[to] = make_float2(exponent, sum);
+      }
+    }
+  }
+}
+
+template <class E, class C, Look kLook>
+void launch_look(const Args &a, unsigned workgroups, hipStream_t stream) {
+  if constexpr (kLook == kElements) {
+    kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+  } else {
+    if (a.d <= 64) kernel<E, C, 64, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+    else if (a.d <= 128) kernel<E, C, 128, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+    else kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+  }
+}
+template <class E, class C> void launch_cache(const Args &a, unsigned workgroups, hipStream_t stream) {
+  // whole 16-byte chunks of a row, 8 bytes at its end in an 8-bit cache
+  constexpr int kSize = sizeof(typename C::elem), kEven = is_8bit<C>::value ? 8 : 16 / kSize;
+  const bool chunks = a.d % kEven == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & (kEven * kSize - 1)) == 0;
+  if (!chunks) launch_look<E, C, kElements>(a, workgroups, stream);
+  else if (a.map.page.d % 16 == 0) launch_look<E, C, kInPage>(a, workgroups, stream);
+  else launch_look<E, C, kPerKey>(a, workgroups, stream);
+}
+template <class E> void launch_queries(const Args &a, va_cache_format format, unsigned workgroups, hipStream_t stream) {
+  if (format == VA_CACHE_I8) launch_cache<E, I8>(a, workgroups, stream);
+  else if (format == VA_CACHE_E4M3) launch_cache<E, E4m3>(a, workgroups, stream);
+  else launch_cache<E, E>(a, workgroups, stream);
+}
+void launch_bf16(const Args &a, va_cache_format format, unsigned workgroups, hipStream_t stream);
+void launch_f16(const Args &a, va_cache_format format, unsigned workgroups, hipStream_t stream);
+void launch_f32(const Args &a, va_cache_format format, unsigned workgroups, hipStream_t stream);
+
+}  // namespace paged
+}  // namespace va

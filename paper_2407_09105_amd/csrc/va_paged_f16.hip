@@ -1,0 +1,6 @@
+// Attention of one token over the key-value cache, queries in f16 (va_paged.h).
+#include "va_paged.h"
+
+void va::paged::launch_f16(const Args &a, va_cache_format format, unsigned workgroups, hipStream_t stream) {
+  launch_queries<F16>(a, format, workgroups, stream);
+}

@@ -28,7 +28,7 @@ def _cache(**kw):
 BAD_CACHES = [
     (2, dict(n_pages=0)), (2, dict(page_size=0)), (2, dict(hkv=-1)), (2, dict(d=0)), (2, dict(n_seqs=-1)), (2, dict(max_pages=-1)),
     (2, dict(table_stride=3)), (2, dict(table_stride=-4)), (2, dict(n_pages=1 << 26)), (2, dict(n_pages=2 ** 31 - 1, hkv=65535)),
-    (2, dict(max_pages=1 << 27, table_stride=1 << 27)), (2, dict(page_size=1 << 20)), (3, dict(d=257)), (3, dict(format=3)), (3, dict(n_seqs=65536)),
+    (2, dict(max_pages=1 << 27, table_stride=1 << 27)), (2, dict(max_pages=2 ** 31 - 1023, page_size=1, table_stride=1 << 31)), (2, dict(page_size=1 << 20)), (3, dict(d=257)), (3, dict(format=3)), (3, dict(n_seqs=65536)),
     (3, dict(hkv=65536)), (1, dict(k=None)), (1, dict(v=None)), (1, dict(page_table=None)),
     (1, dict(format=binding.CACHE_I8, k_scale=None)), (1, dict(format=binding.CACHE_E4M3, v_scale=None))]
 
@@ -63,6 +63,19 @@ def test_attention_arguments(L):
     assert with_(0, None) == with_(1, None) == with_(2, None) == with_(4, None) == with_(6, None) == 1
     assert with_(3, 7) == 3 and with_(5, 3) == 2 and with_(5, 0) == 2 and with_(5, 65536) == 3
     assert with_(4, C.byref(_cache(n_seqs=0))) == 0
+    # one long sequence: shared by many workgroups, which need room
+    long = _cache(n_pages=10000, n_seqs=1, max_pages=10000, table_stride=10000)
+    need = L.va_paged_attn_workspace_bytes(1, 10000, 16, 4, 2, 64)
+    assert need > 0 and need % 256 == 0
+    ok[4] = C.byref(long)
+    assert with_(9, need - 1) == 4 and with_(8, None) == 1 and with_(8, P + 4) == 4
+
+
+def test_workspace_sizes(L):
+    f = L.va_paged_attn_workspace_bytes
+    assert f(0, 4, 16, 4, 2, 64) == f(3, 0, 16, 4, 2, 64) == f(3, 4, 16, 4, 2, 0) == f(3, 4, -1, 4, 2, 64) == 0
+    assert f(5, 4, 16, 4, 2, 64) == 0                                # short contexts are not cut
+    assert f(65535, 1 << 10, 1 << 10, 64, 8, 128) < 8 << 30          # and none takes the card's memory
 
 
 @pytest.mark.filterwarnings("ignore:Accessing the data pointer")
