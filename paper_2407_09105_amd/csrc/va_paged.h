@@ -33,14 +33,20 @@ struct Split {
 };
 Split split_of(int n_seqs, long long capacity, int hq, int hkv);
 
-// Parts of all sequences in order: [slots, hq, d] sums of P V, then [slots, hq] pairs (reference exponent, sum of P).
+// Of every sequence where its parts begin and how many it has; then of all parts in order [slots, hq] pairs (reference exponent,
+// sum of P) and [slots, hq, d] sums of P V.
 struct Workspace {
-  float *o;
+  int2 *parts;
   float2 *ml;
+  float *o;
 };
-static inline Workspace workspace(float *p, const Split &s, int hq, int d) {
-  const size_t n = (size_t)s.slots * hq * d;
-  return {p, (float2 *)(p + (n + 1) / 2 * 2)};
+static inline size_t workspace_bytes(const Split &s, int n_seqs, int hq, int d) {
+  return s.slots == n_seqs ? 0 : (size_t)n_seqs * sizeof(int2) + (size_t)s.slots * hq * (sizeof(float2) + d * sizeof(float));
+}
+static inline Workspace workspace(void *p, const Split &s, int n_seqs, int hq) {
+  int2 *const parts = (int2 *)p;
+  float2 *const ml = (float2 *)(parts + n_seqs);
+  return {parts, ml, (float *)(ml + (size_t)s.slots * hq)};
 }
 
 struct Part {
@@ -49,16 +55,14 @@ struct Part {
   int n;                // tokens of the sequence
 };
 
-// The part that a slot holds, false where it holds none; with slot < 0 the first part of sequence seq.  A sequence of u units has max(1, ceil(u / c)) parts of c units, where
+// The part that a slot holds; false where it holds none.  A sequence of u units has max(1, ceil(u / c)) parts of c units, where
 // c = max(least_units, ceil(all units / (slots - n_seqs))): no more than slots in all, whatever the lengths are, and of equal
 // size but for the last of each sequence.  A wave reads 64 lengths at a time and adds them up across its lanes.
-__device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, const PageMap &map, const Split &split, int slot, int seq,
-                                          Part &part) {
+__device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, const PageMap &map, const Split &split, int slot, Part &part) {
   const int lane = threadIdx.x & 63, B = map.n_seqs;
   auto length = [&](int b) { return b < B ? min(max(lens[b], 0), map.capacity) : 0; };
   if (split.slots == B) {
-    seq = slot < 0 ? seq : slot;
-    part = {seq, seq, 1, 0x7fffffff / kUnit, uniform(length(seq))};
+    part = {slot, slot, 1, 0x7fffffff / kUnit, uniform(length(slot))};
     return true;
   }
   double total = 0;  // exact: below 2^53
@@ -81,7 +85,7 @@ __device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, cons
       const int x = __shfl_up(upto, o);
       if (lane >= o) upto += x;
     }
-    const uint64_t past = slot < 0 ? __ballot(b0 + lane >= seq) : __ballot(before + upto > slot);
+    const uint64_t past = __ballot(before + upto > slot);
     if (past) {
       const int at = __builtin_ctzll(past);
       part = {b0 + at, before + __builtin_amdgcn_readlane(upto - parts, at), __builtin_amdgcn_readlane(parts, at), c,
@@ -269,7 +273,7 @@ kernel(Args a) {
   if (pair >= a.split.slots * hkv) return;
   const int slot = pair / hkv, g = pair - slot * hkv;
   Part part;
-  if (!find_part(a.lens, map, a.split, slot, 0, part)) return;
+  if (!find_part(a.lens, map, a.split, slot, part)) return;
   const int b = part.b, n = part.n;
   const int heads = min(G - head0, kHeads);  // rows of this workgroup
   const size_t first_head = (size_t)b * a.hq + g * G + head0;
@@ -560,6 +564,9 @@ kernel(Args a) {
     }
     now = next;
   }
+
+  if (a.split.slots != map.n_seqs && slot == part.first && g == 0 && head0 == 0 && threadIdx.x == 0)
+    a.ws.parts[b] = make_int2(part.first, part.parts);
 
   // ---- the waves' results: relative to the largest reference, added in order ----
   l_run = head_sum(l_run);

@@ -21,53 +21,96 @@ Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
 
 namespace {
 
-// One workgroup per (sequence, query head): the parts' sums, relative to the largest reference exponent, added in order.
-template <class E>
+// One workgroup per (sequence, query head) adds up the parts' sums, weighted relative to the largest reference exponent: every
+// kJoinRows-th part one group of threads', a column each, and then the groups' sums in order.
+constexpr int kMostParts = kWorkgroups + 1;  // of one sequence
+
+template <class E, int kCols>  // kCols: threads of a group, d rounded up to 64, 128 or 256
 __global__ void __launch_bounds__(kThreads)
-join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, const int32_t *__restrict__ lens, PageMap map,
-            Split split, int hq, int d) {
-  const int b = blockIdx.x, head = blockIdx.y;
-  Part part;
-  if (!find_part(lens, map, split, -1, b, part) || part.parts == 1) return;
-  const float2 *const ml = ws.ml + (size_t)part.first * hq + head;
-  const float *const o = ws.o + ((size_t)part.first * hq + head) * d;
+join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d) {
+  constexpr int kJoinRows = kThreads / kCols, kFly = 8;  // parts in flight
+  __shared__ float weight[kMostParts], some[2][kThreads];
+  const int b = blockIdx.x, head = blockIdx.y, t = threadIdx.x;
+  const int2 of = ws.parts[b];
+  const int first = of.x, parts = of.y;
+  if (parts == 1) return;  // its only workgroup has written the result
+  const float2 *const ml = ws.ml + (size_t)first * hq + head;
+  float2 mine[(kMostParts + kThreads - 1) / kThreads];
   float top = -INFINITY;
-  for (int x = 0; x < part.parts; ++x) top = fmaxf(top, ml[(size_t)x * hq].x);
-  float sum = 0.f, y = 0.f;
-  const int c = threadIdx.x;
-  for (int x = 0; x < part.parts; ++x) {
-    const float2 one = ml[(size_t)x * hq];
-    const float weight = one.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(one.x - top);
-    sum += weight * one.y;
-    if (c < d) y += weight * o[(size_t)x * hq * d + c];
+#pragma unroll
+  for (int k = 0; k * kThreads < kMostParts; ++k) {
+    const int x = t + k * kThreads;
+    mine[k] = x < parts ? ml[(size_t)x * hq] : make_float2(-INFINITY, 0.f);
+    top = fmaxf(top, mine[k].x);
   }
-  if (c < d) O[((size_t)b * hq + head) * d + c] = (typename E::elem)(sum != 0.f ? y / sum : 0.f);
-  if (c == 0) LSE[(size_t)head * map.n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  if (t % 64 == 0) some[0][t / 64] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(some[0][0], some[0][1]), fmaxf(some[0][2], some[0][3]));
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k * kThreads < kMostParts; ++k) {
+    const int x = t + k * kThreads;
+    const float w = mine[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[k].x - top);
+    if (x < parts) weight[x] = w;
+    sum += w * mine[k].y;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+  if (t % 64 == 0) some[1][t / 64] = sum;
+  __syncthreads();
+  sum = some[1][0] + some[1][1] + some[1][2] + some[1][3];
+  const int c = t % kCols;
+  const float *const o = ws.o + ((size_t)first * hq + head) * d + min(c, d - 1);
+  float y = 0.f;
+  for (int x0 = t / kCols; x0 < parts; x0 += kJoinRows * kFly) {
+    float v[kFly];
+#pragma unroll
+    for (int k = 0; k < kFly; ++k) v[k] = o[(size_t)min(x0 + k * kJoinRows, parts - 1) * hq * d];
+#pragma unroll
+    for (int k = 0; k < kFly; ++k)
+      if (x0 + k * kJoinRows < parts) y += weight[x0 + k * kJoinRows] * v[k];
+  }
+  if constexpr (kJoinRows > 1) {
+    __syncthreads();  // both of `some` are read
+    some[0][t] = y;
+    __syncthreads();
+    y = 0.f;
+#pragma unroll
+    for (int k = 0; k < kJoinRows; ++k) y += some[0][k * kCols + c];
+  }
+  if (t < d) O[((size_t)b * hq + head) * d + t] = (typename E::elem)(sum != 0.f ? y / sum : 0.f);
+  if (t == 0) LSE[(size_t)head * n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <class E> void launch_join(void *O, float *LSE, const Workspace &ws, int n_seqs, int hq, int d, hipStream_t stream) {
+  const dim3 grid((unsigned)n_seqs, (unsigned)hq);
+  typename E::elem *const o = (typename E::elem *)O;
+  if (d <= 64) join_kernel<E, 64><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+  else if (d <= 128) join_kernel<E, 128><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+  else join_kernel<E, 256><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
 }
 
 }  // namespace
 }  // namespace paged
 
 size_t paged_workspace_bytes(int n_seqs, long long capacity, int hq, int hkv, int d) {
-  const paged::Split s = paged::split_of(n_seqs, capacity, hq, hkv);
-  return s.slots == n_seqs ? 0 : ((size_t)s.slots * hq * d + 1) / 2 * 2 * sizeof(float) + (size_t)s.slots * hq * sizeof(float2);
+  return paged::workspace_bytes(paged::split_of(n_seqs, capacity, hq, hkv), n_seqs, hq, d);
 }
 
 hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache &c, int hq, const int32_t *lens, float scale,
                         float *work, hipStream_t stream) {
   using namespace paged;
   const Split split = split_of(c.n_seqs, (long long)c.max_pages * c.page_size, hq, c.hkv);
-  const Workspace ws = workspace(work, split, hq, c.d);
+  const Workspace ws = workspace(work, split, c.n_seqs, hq);
   const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, hq, c.d, scale * 1.4426950408889634f};
   const long long groups = ceil_div(hq / c.hkv, kHeads), workgroups = ((long long)split.slots * c.hkv + 7) / 8 * 8 * groups;
   if (workgroups > 0x7fffffffll) return hipErrorInvalidValue;
   (dt == VA_BF16 ? launch_bf16 : dt == VA_F16 ? launch_f16 : launch_f32)(a, c.format, (unsigned)workgroups, stream);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || split.slots == c.n_seqs) return e;
-  const dim3 grid((unsigned)c.n_seqs, (unsigned)hq);
-  if (dt == VA_BF16) join_kernel<Bf16><<<grid, kThreads, 0, stream>>>((__bf16 *)O, LSE, ws, lens, a.map, split, hq, c.d);
-  else if (dt == VA_F16) join_kernel<F16><<<grid, kThreads, 0, stream>>>((_Float16 *)O, LSE, ws, lens, a.map, split, hq, c.d);
-  else join_kernel<F32><<<grid, kThreads, 0, stream>>>((float *)O, LSE, ws, lens, a.map, split, hq, c.d);
+  (dt == VA_BF16 ? launch_join<Bf16> : dt == VA_F16 ? launch_join<F16> : launch_join<F32>)(O, LSE, ws, c.n_seqs, hq, c.d, stream);
   return hipGetLastError();
 }
 
