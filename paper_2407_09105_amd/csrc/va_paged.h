@@ -30,6 +30,7 @@ constexpr float kLazyLog2 = 8.f;
 struct Split {
   int slots;        // room for parts; n_seqs where no sequence is cut
   int least_units;  // least length of a part
+  FastDiv extra;    // slots - n_seqs
 };
 Split split_of(int n_seqs, long long capacity, int hq, int hkv);
 
@@ -55,44 +56,51 @@ struct Part {
   int n;                // tokens of the sequence
 };
 
+// Sum of a wave's values up to each lane: shifts within rows of 16, then the rows' totals (data-parallel primitives, no LDS).
+__device__ __forceinline__ int sum_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // last lane of row 0 / 2 to row 1 / 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+  return x;
+}
+
 // The part that a slot holds; false where it holds none.  A sequence of u units has max(1, ceil(u / c)) parts of c units, where
 // c = max(least_units, ceil(all units / (slots - n_seqs))): no more than slots in all, whatever the lengths are, and of equal
 // size but for the last of each sequence.  A wave reads 64 lengths at a time and adds them up across its lanes.
 __device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, const PageMap &map, const Split &split, int slot, Part &part) {
   const int lane = threadIdx.x & 63, B = map.n_seqs;
-  auto length = [&](int b) { return b < B ? min(max(lens[b], 0), map.capacity) : 0; };
+  auto length = [&](int b) { return min(max(lens[min(b, B - 1)], 0), map.capacity); };
   if (split.slots == B) {
+    if (slot >= B) return false;
     part = {slot, slot, 1, 0x7fffffff / kUnit, uniform(length(slot))};
     return true;
   }
-  double total = 0;  // exact: below 2^53
-  int mine = 0;
-  for (int b0 = 0; b0 < B; b0 += 64) {
-    mine = length(b0 + lane);
-    total += (double)((mine + kUnit - 1) / kUnit);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
-  const int c = uniform(max(split.least_units, (int)fmin(ceil(total / (split.slots - B)), 0x7fffffff / kUnit)));
+  const int mine0 = length(lane);
+  auto units_of = [](int n) { return (int)((uint32_t)(n + kUnit - 1) / kUnit); };
+  auto units_at = [&](int b0, int n) { return b0 + lane < B ? units_of(n) : 0; };
+  long long total = __builtin_amdgcn_readlane(sum_upto(units_at(0, mine0)), 63);  // 64 x 2^24 at most
+  for (int b0 = 64; b0 < B; b0 += 64) total += __builtin_amdgcn_readlane(sum_upto(units_at(b0, length(b0 + lane))), 63);
+  const int drop = total >= 1 << 30 ? 10 : 0;  // to what a 32-bit division takes, rounded up
+  const int c = max(split.least_units, (((int)((total + (1 << drop) - 1) >> drop) + (int)split.extra.d - 1) / split.extra) << drop);
+  const float inv = 1.f / (float)c;
   int before = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
-    if (B > 64) mine = length(b0 + lane);
-    const int units = (mine + kUnit - 1) / kUnit;
-    const int parts = b0 + lane < B ? max(1, (units + c - 1) / c) : 0;
-    int upto = parts;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
-    const uint64_t past = __ballot(before + upto > slot);
+    const int mine = b0 == 0 ? mine0 : length(b0 + lane), units = units_of(mine);
+    int parts = (int)((float)units * inv);  // units <= 2^24 are exact, the quotient is off by one at most
+    const int rest = units - parts * c;
+    parts += rest > c ? 2 : rest > 0 ? 1 : 0;
+    parts = b0 + lane < B ? max(1, parts) : 0;
+    const int upto = before + sum_upto(parts);
+    const uint64_t past = __ballot(upto > slot);
     if (past) {
-      const int at = __builtin_ctzll(past);
-      part = {b0 + at, before + __builtin_amdgcn_readlane(upto - parts, at), __builtin_amdgcn_readlane(parts, at), c,
-              __builtin_amdgcn_readlane(mine, at)};
+      const int at = __builtin_ctzll(past), has = __builtin_amdgcn_readlane(parts, at);
+      part = {b0 + at, __builtin_amdgcn_readlane(upto, at) - has, has, c, __builtin_amdgcn_readlane(mine, at)};
       return true;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    before = __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
 }
@@ -188,7 +196,8 @@ struct Args {
   const int32_t *lens;
   Split split;
   Workspace ws;
-  int hq, d;
+  FastDiv hkv, groups;  // KV heads; groups of kHeads query heads of one KV head
+  int hq, G, d;         // G = hq / hkv
   float scale_log2;
 };
 
@@ -265,13 +274,12 @@ kernel(Args a) {
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), i = lane & 15, h = lane >> 4;
   const PageMap &map = a.map;
-  const int hkv = map.hkv, d = a.d, G = a.hq / hkv, page = map.page.d;
+  const int hkv = map.hkv, d = a.d, G = a.G, page = map.page.d;
 
   // Workgroup ids go to the 8 XCDs in turn: the groups of 16 query heads of one KV head, which read the same keys, 8 ids apart.
-  const int groups = (G + kHeads - 1) / kHeads, turn = blockIdx.x >> 3;
-  const int pair = turn / groups * 8 + (blockIdx.x & 7), head0 = turn % groups * kHeads;
+  const int turn = blockIdx.x >> 3, pair = turn / a.groups * 8 + (blockIdx.x & 7), head0 = turn % a.groups * kHeads;
   if (pair >= a.split.slots * hkv) return;
-  const int slot = pair / hkv, g = pair - slot * hkv;
+  const int slot = pair / a.hkv, g = pair - slot * hkv;
   Part part;
   if (!find_part(a.lens, map, a.split, slot, part)) return;
   const int b = part.b, n = part.n;
@@ -281,7 +289,7 @@ kernel(Args a) {
   // q as operand B: head i, the columns of the K chunks
   constexpr int kQf = kF32 ? kKn * kCpc : kKn * kCpc / 8;
   typename std::conditional<kF32, float, qx8>::type qf[kQf];
-  {
+  if constexpr (kLook == kElements) {
     const elem *q = (const elem *)a.Q + (first_head + min(i, heads - 1)) * d;
     auto q_at = [&](int column) { return i < heads && column < d ? q[min(column, d - 1)] : (elem)0.f; };
 #pragma unroll
@@ -292,6 +300,22 @@ kernel(Args a) {
         if constexpr (kF32) qf[x * kCpc + e] = y;
         else qf[(x * kCpc + e) / 8][e % 8] = y;
       }
+  } else {
+    constexpr int kEach = 16 / (int)sizeof(elem);
+    const buffer_t q = make_buffer((const elem *)a.Q + first_head * d, (size_t)heads * d * sizeof(elem));  // no rows behind `heads`
+#pragma unroll
+    for (int x = 0; x < kKn; ++x)
+#pragma unroll
+      for (int e = 0; e < kCpc; e += kEach) {
+        const int column = (4 * x + h) * kCpc + e;
+        const u32x4 y = buffer_load16(q, column < d ? (uint32_t)((i * d + column) * sizeof(elem)) : kPastEnd);
+        if constexpr (kF32) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) qf[x * kCpc + e + v] = __uint_as_float(y[v]);
+        } else {
+          qf[(x * kCpc + e) / 8] = as_x8<E16>(y);
+        }
+      }
   }
 
   // keys j0 .. j1 - 1, tiles wave, wave + kWaves, ...
@@ -300,21 +324,31 @@ kernel(Args a) {
   const int tile_end = (j1 + kTile - 1) / kTile;
   const int32_t *const table = map.table + (int64_t)b * map.stride;
 
-  // ---- rows of a tile ----
-  struct Rows {
-    int row[2];    // kInPage: row of the product's first key; else of this lane's key i; its scales
-    int count[2];  // kInPage: keys that exist; else 1 or 0 for key i
+  // ---- rows of a tile: the entries are requested two tiles ahead, the rows one ----
+  struct Entries {
+    int j[2], at[2], id[2];  // key (kInPage: the product's first, else this lane's own), the page's place in the table, the page
   };
-  auto find_rows = [&](int tile) {
+  struct Rows {
+    int row[2];    // of that key; row 0 where it does not exist (kInPage: not read then)
+    int count[2];  // keys that exist, kInPage: of the product's 16, else of this lane's one
+  };
+  auto entries = [&](int tile) {
+    Entries t;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      t.j[s] = tile * kTile + 16 * s + (kLook == kInPage ? 0 : i);
+      t.at[s] = min(t.j[s], j1 - 1) / map.page;
+      t.id[s] = table[t.at[s]];
+    }
+    return t;
+  };
+  auto rows_of = [&](const Entries &t) {
     Rows r;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int j = tile * kTile + 16 * s + (kLook == kInPage ? 0 : i);
-      int at = 0, id = -1;
-      if ((uint32_t)j < (uint32_t)j1) at = j / map.page, id = table[at];
-      const bool ok = (uint32_t)id < (uint32_t)map.n_pages;
-      r.row[s] = ok ? (id * hkv + g) * page + (j - at * page) : 0;
-      r.count[s] = !ok ? 0 : kLook == kInPage ? min(j1 - j, 16) : 1;
+      const bool ok = t.j[s] < j1 && (uint32_t)t.id[s] < (uint32_t)map.n_pages;
+      r.row[s] = ok ? (t.id[s] * hkv + g) * page + (t.j[s] - t.at[s] * page) : 0;
+      r.count[s] = !ok ? 0 : kLook == kInPage ? min(j1 - t.j[s], 16) : 1;
     }
     return r;
   };
@@ -433,19 +467,27 @@ kernel(Args a) {
   float m_ref = -INFINITY, m_thr = -INFINITY;  // raw score that exponents are relative to, and the one that moves it
   float l_run = 0.f;                           // this lane's share of the sum of P
 
+  // In flight: the entries of tile + 2 kWaves, the keys of tile + kWaves, the values of tile.  Behind the last tile no key exists;
+  // its loads are made all the same (a branch around them would make the compiler wait for all that is in flight).
   int tile = j0 / kTile + wave;
-  Rows now = find_rows(tile);
-  if (tile < tile_end) load_k(now);
+  Rows now = {};
+  Entries ahead = {};
+  if (tile < tile_end) {
+    now = rows_of(entries(tile));
+    load_k(now);
+    ahead = entries(tile + kWaves);
+  }
   for (; tile < tile_end; tile += kWaves) {
-    const Rows next = find_rows(tile + kWaves);  // no keys behind the last tile
+    const Rows next = rows_of(ahead);
+    ahead = entries(tile + 2 * kWaves);
     load_v(now);
+    __builtin_amdgcn_sched_barrier(0);  // they are on their way before the keys are waited for
     // ---- S^T = K Q^T ----
-    f32x4 s[2];
+    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < kKn; ++x) {
 #pragma unroll
-      for (int x = 0; x < kKn; ++x) {
+      for (int t = 0; t < 2; ++t) {
         const KPiece &p = kr[t][x];
         if constexpr (kF32 && k8) {
 #pragma unroll
@@ -470,9 +512,12 @@ kernel(Args a) {
           s[t] = mfma16(as_x8<E16>(u32x4{p.x[0], p.x[1], p.x[2], p.x[3]}), qf[x], s[t]);
         }
       }
-      if constexpr (k8) s[t] *= ksr[t];
     }
-    if (tile + kWaves < tile_end) load_k(next);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if constexpr (k8) s[t] *= ksr[t];
+    load_k(next);
+    __builtin_amdgcn_sched_barrier(0);
     // ---- keys that do not exist ----
     if constexpr (kLook == kInPage) {
       if (now.count[0] + now.count[1] < kTile) {
@@ -619,7 +664,7 @@ void launch_look(const Args &a, unsigned workgroups, hipStream_t stream) {
 template <class E, class C> void launch_cache(const Args &a, unsigned workgroups, hipStream_t stream) {
   // whole 16-byte chunks of a row, 8 bytes at its end in an 8-bit cache
   constexpr int kSize = sizeof(typename C::elem), kEven = is_8bit<C>::value ? 8 : 16 / kSize;
-  const bool chunks = a.d % kEven == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & (kEven * kSize - 1)) == 0;
+  const bool chunks = a.d % kEven == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & (kEven * kSize - 1)) == 0 && ((uintptr_t)a.Q & 3) == 0;
   if (!chunks) launch_look<E, C, kElements>(a, workgroups, stream);
   else if (a.map.page.d % 16 == 0) launch_look<E, C, kInPage>(a, workgroups, stream);
   else launch_look<E, C, kPerKey>(a, workgroups, stream);

@@ -15,8 +15,9 @@ Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
   const int groups = ceil_div(hq / hkv, kHeads);
   const long long least = kLeastUnits * kUnit, most = n_seqs * ((capacity + least - 1) / least);  // parts that there can be
   const long long room = (kWorkgroups + (long long)hkv * groups - 1) / ((long long)hkv * groups);
-  if (capacity <= least) return {n_seqs, kLeastUnits};
-  return {n_seqs + (int)std::min(room, most), kLeastUnits};
+  if (capacity <= least) return {n_seqs, kLeastUnits, fast_div(1)};
+  const int extra = (int)std::min(room, most);
+  return {n_seqs + extra, kLeastUnits, fast_div(extra)};
 }
 
 namespace {
@@ -104,8 +105,10 @@ hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const v
   using namespace paged;
   const Split split = split_of(c.n_seqs, (long long)c.max_pages * c.page_size, hq, c.hkv);
   const Workspace ws = workspace(work, split, c.n_seqs, hq);
-  const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, hq, c.d, scale * 1.4426950408889634f};
-  const long long groups = ceil_div(hq / c.hkv, kHeads), workgroups = ((long long)split.slots * c.hkv + 7) / 8 * 8 * groups;
+  const int G = hq / c.hkv, groups = ceil_div(G, kHeads);
+  const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, fast_div(c.hkv), fast_div(groups), hq, G, c.d,
+                  scale * 1.4426950408889634f};
+  const long long workgroups = ((long long)split.slots * c.hkv + 7) / 8 * 8 * groups;
   if (workgroups > 0x7fffffffll) return hipErrorInvalidValue;
   (dt == VA_BF16 ? launch_bf16 : dt == VA_F16 ? launch_f16 : launch_f32)(a, c.format, (unsigned)workgroups, stream);
   const hipError_t e = hipGetLastError();
