@@ -5,7 +5,7 @@ forward, backward) runs in the library's HIP kernels.  PyTorch supplies device
 memory and the stream.  There is no fallback: if the library is missing, or a
 call returns a non-zero status, an exception is raised.
 
-The plain calls of boundaries, forward and backward (outputs not given) marshal in C++
+The plain calls of boundaries, forward, backward and the key-value cache (outputs not given) marshal in C++
 (_va_native, which returns None where it leaves a call to the code here); everything else goes through ctypes, and so
 do those where _va_native was not built for the interpreter and torch that run.
 """
@@ -103,6 +103,8 @@ def lib() -> C.CDLL:
     _native = _load_native()
     if _native is not None:
         _native.connect(*native_addresses(L))
+        _native.connect_cache(*(C.cast(getattr(L, name), C.c_void_p).value for name in (
+            "va_cache_write", "va_cache_read", "va_paged_attn_workspace_bytes", "va_paged_attn_fwd")))
     _lib = L
     return L
 
@@ -116,9 +118,10 @@ def _load_native():
         why = str(e)
     else:
         built_for = getattr(native, "torch_version", "another version")
-        if built_for == torch.__version__:
+        if built_for == torch.__version__ and hasattr(native, "connect_cache"):
             return native
-        why = f"built for torch {built_for}, this is {torch.__version__}"
+        why = (f"built for torch {built_for}, this is {torch.__version__}" if built_for != torch.__version__
+               else "it is older than this binding")
     logging.getLogger(__name__).warning("calls go through ctypes (%s); run __graft_entry__.build() "
                                         "(python paper_2407_09105_amd/build.py)", why)
     return None
@@ -444,6 +447,9 @@ _CACHE_FORMATS = {torch.float32: CACHE_PLAIN, torch.bfloat16: CACHE_PLAIN, torch
                   torch.float8_e4m3fn: CACHE_E4M3}
 
 
+_ROW_TYPES = {torch.float32: VA_F32, torch.bfloat16: VA_BF16, torch.float16: VA_F16}
+
+
 def paged_cache(n_pages: int, page_size: int, hkv: int, d: int, dtype: torch.dtype, device="cuda") -> PagedCache:
     """An empty cache (zeros).  dtype: that of K and V, or int8 or float8_e4m3fn, whose rows also carry a float32 scale."""
     if dtype not in _CACHE_FORMATS:
@@ -508,6 +514,11 @@ def paged_cache_write(k: torch.Tensor, v: torch.Tensor, cache, page_table: torch
     sequence seq_ids[t] (int32; default: t), whose pages are row seq_ids[t] of page_table (int32, [sequences, pages]).  A packed
     stream of prompts brings its position ids and Segments.seg_id.  Rows are quantised if the cache is int8 or float8_e4m3fn.
     Tokens without a place (no such sequence, position or page) are left out.  Enqueues one kernel."""
+    lib()
+    if _native is not None and k.is_cuda:
+        got = _native.cache_write(k, v, cache, page_table, position_ids, seq_ids, torch.cuda.current_device(), _stream())
+        if got is not None:
+            return _check("va_cache_write", got)
     _check("va_cache_write", lib().va_cache_write(k.data_ptr(), v.data_ptr(),
                                                   *_cache_rows(k, v, cache, page_table, position_ids, seq_ids), _stream()))
 
@@ -516,9 +527,15 @@ def paged_cache_read(cache, page_table: torch.Tensor, position_ids: torch.Tensor
                      dtype: Optional[torch.dtype] = None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """-> K, V [N, Hkv, d]: the cached rows of the tokens that position_ids and seq_ids name as in paged_cache_write, zeros where there
     is none.  dtype: of the rows out of an 8-bit cache (default bfloat16).  out: the two tensors to fill.  Enqueues one kernel."""
+    lib()
     pages = cache[0]
     if out is None:
         dtype = dtype or (torch.bfloat16 if _CACHE_FORMATS.get(pages.dtype) else pages.dtype)
+        if _native is not None and pages.is_cuda and dtype in _ROW_TYPES:
+            got = _native.cache_read(cache, page_table, position_ids, seq_ids, _ROW_TYPES[dtype], torch.cuda.current_device(), _stream())
+            if got.__class__ is tuple:
+                return got
+            _check("va_cache_read", got or VA_OK)
         k, v = (torch.empty((position_ids.numel(), pages.shape[1], pages.shape[-1]), dtype=dtype, device=pages.device) for _ in "kv")
     else:
         k, v = out
@@ -534,6 +551,12 @@ def paged_attn_fwd(q: torch.Tensor, cache, page_table: torch.Tensor, context_len
     """One token of every sequence against its cached keys and values: q [B, Hq, d], page_table int32 [B, pages], context_lens int32
     [B] (cached tokens, the new one's own included) -> O [B, Hq, d] (dtype of q), LSE [Hq, B] float32.  An empty sequence gives zeros
     and -inf.  workspace: float32, of paged_attn_workspace(...)'s size, one for each of several calls that may overlap."""
+    lib()
+    if _native is not None and out is None and lse is None and workspace is None and q.is_cuda:
+        got = _native.paged(q, cache, page_table, context_lens, float(softmax_scale), torch.cuda.current_device(), _stream())
+        if got.__class__ is tuple:
+            return got
+        _check("va_paged_attn_fwd", got or VA_OK)
     c = _kv_cache(cache, page_table, q.dtype, q, context_lens)
     if q.dim() != 3 or q.shape[2] != c.d or q.shape[0] != c.n_seqs or q.shape[1] % max(c.hkv, 1) or context_lens.shape != (c.n_seqs,):
         raise ValueError(f"expected Q [{c.n_seqs}, a multiple of {c.hkv}, {c.d}] and {c.n_seqs} context lengths")

@@ -393,3 +393,46 @@ def test_results_do_not_change_from_call_to_call():
     for _ in range(5):
         again = s.attend()
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("kind", ["plain", "i8", "e4m3"])
+def test_cpp_marshalling_takes_the_plain_calls(kind, monkeypatch):
+    """The calls of a decoding step marshal in C++ and give what the ctypes calls give; what differs goes through Python."""
+    s = Setup("bf16", kind, 8, 2, 64, 16, [40, 300, 0], seed=31, garbage=False, width=24, spare=8)
+    k, v = _rows(3, 2, 64, "bf16", 7)
+    native, taken = binding._native, []
+    assert native is not None
+
+    class Spy:
+        def __getattr__(self, name):
+            def call(*args):
+                got = getattr(native, name)(*args)
+                taken.append((name, type(got).__name__))
+                return got
+            return call
+
+    def step(cache):
+        binding.paged_cache_write(k, v, cache, s.table, s.lens)
+        rows = binding.paged_cache_read(cache, s.table, s.lens, torch.arange(3, dtype=torch.int32, device=DEV), dtype=torch.bfloat16)
+        return (*rows, *binding.paged_attn_fwd(s.q, cache, s.table, s.lens + 1), *(x for x in cache if x is not None))
+
+    monkeypatch.setattr(binding, "_native", Spy())
+    caches = [tuple(x if x is None else x.clone() for x in s.cache) for _ in range(3)]
+    got = step(binding.PagedCache(*caches[0]))
+    assert taken == [("cache_write", "int"), ("cache_read", "tuple"), ("paged", "tuple")]
+    del taken[:]
+    lists = step(list(caches[1]))       # no tuple
+    assert [t for _, t in taken] == ["NoneType"] * 3
+    monkeypatch.setattr(binding, "_native", None)
+    for a, b, c in zip(got, step(caches[2]), lists):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+    # errors are the same with and without it
+    for n in (native, None):
+        monkeypatch.setattr(binding, "_native", n)
+        with pytest.raises(ValueError, match="multiple"):
+            binding.paged_attn_fwd(torch.zeros(3, 5, 64, device=DEV, dtype=torch.bfloat16), s.cache, s.table, s.lens)
+        with pytest.raises(TypeError):
+            binding.paged_attn_fwd(s.q, s.cache, s.table, s.lens.long())
+        with pytest.raises(binding.VarlenAttnError, match="unsupported"):
+            wide = tuple(torch.zeros(4, 1, 16, 264, device=DEV, dtype=torch.bfloat16) for _ in "kv") + (None, None)
+            binding.paged_attn_fwd(torch.zeros(3, 1, 264, device=DEV, dtype=torch.bfloat16), wide, s.table, s.lens)
