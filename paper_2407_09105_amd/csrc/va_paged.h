@@ -182,8 +182,8 @@ template <> struct shift_log2<F16> { static constexpr float value = 6.f; };
 // ---- the kernel ---------------------------------------------------------------------------------------
 
 // How a tile's rows are found: kInPage: page_size is a multiple of 16, and the 16 keys of a product lie next to each other; kPerKey:
-// each key on its own; kElements: likewise, and rows are read element by element (head dims or addresses that 16-byte chunks do not
-// fit).
+// each key on its own; kElements: likewise, and rows are read in dwords or single elements (head dims or addresses that 16-byte
+// chunks do not fit).
 enum Look { kInPage, kPerKey, kElements };
 
 struct Args {
@@ -226,10 +226,15 @@ template <int kBytes> __device__ __forceinline__ Piece<kBytes> memory_piece(cons
   for (int i = 0; i < kBytes / 4; ++i) q.x[i] = r.x[i];
   return q;
 }
-// elements `column` .. of a row of d elements, zeros behind it
-template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_piece(const T *row, int column, int d) {
+// elements `column` .. of a row of d elements, zeros behind it; dwords: rows begin and end at whole dwords
+template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_piece(const T *row, int column, int d, bool dwords) {
   constexpr int kEach = 4 / sizeof(T);
   Piece<kBytes> p;
+  if (dwords) {
+#pragma unroll
+    for (int i = 0; i < kBytes / 4; ++i) p.x[i] = column + i * kEach < d ? *(const uint32_t *)(row + column + i * kEach) : 0u;
+    return p;
+  }
 #pragma unroll
   for (int i = 0; i < kBytes / 4; ++i) {
     uint32_t w = 0;
@@ -361,11 +366,15 @@ kernel(Args a) {
   for (int x = 0; x < kHf; ++x) v_off[x] = (16 * x + i) * kVC < d ? (uint32_t)(4 * h * row_bytes + (16 * x + i) * kVBytes) : kPastEnd;
   const bool half_chunk = k8 && (d & 8) != 0;  // rows end in the middle of a 16-byte chunk
 
+  const bool dwords = kLook == kElements && (row_bytes & 3) == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0;
+
   typedef Piece<16> KPiece;
   typedef Piece<kVBytes> VPiece;
   KPiece kr[2][kKn];
   VPiece vr[8][kHf];
+  // scales: kInPage of keys 4 h + 0..3; else of this lane's key, handed round when they are used
   f32x4 ksr[2], vsr[2];
+  float ks_own[2], vs_own[2];
 
   auto load_k = [&](const Rows &r) {
 #pragma unroll
@@ -393,7 +402,7 @@ kernel(Args a) {
         const char *row = (const char *)a.k + (size_t)r.row[s] * row_bytes;  // row 0 for a key that does not exist
         if constexpr (kLook == kElements) {
 #pragma unroll
-          for (int x = 0; x < kKn; ++x) kr[s][x] = element_piece<cached, 16>((const cached *)row, (4 * x + h) * kCpc, d);
+          for (int x = 0; x < kKn; ++x) kr[s][x] = element_piece<cached, 16>((const cached *)row, (4 * x + h) * kCpc, d, dwords);
         } else if (d == kDh) {
 #pragma unroll
           for (int x = 0; x < kKn; ++x) kr[s][x] = memory_piece<16>(row + (4 * x + h) * 16);
@@ -410,10 +419,7 @@ kernel(Args a) {
             }
           }
         }
-        if constexpr (k8) {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) ksr[s][v] = a.ks[__shfl(r.row[s], 4 * h + v)];
-        }
+        if constexpr (k8) ks_own[s] = a.ks[r.row[s]];
       }
     }
   };
@@ -442,7 +448,7 @@ kernel(Args a) {
           if constexpr (kLook == kElements) {
 #pragma unroll
             for (int x = 0; x < kHf; ++x)
-              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, ok ? d : 0);
+              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, ok ? d : 0, dwords);
           } else if (all) {
 #pragma unroll
             for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
@@ -453,8 +459,8 @@ kernel(Args a) {
               if (ok && (16 * x + i) * kVC < d) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
             }
           }
-          if constexpr (k8) vsr[s][v] = ok ? a.vs[from] : 0.f;
         }
+        if constexpr (k8) vs_own[s] = a.vs[r.row[s]];
       }
     }
   };
@@ -513,9 +519,16 @@ kernel(Args a) {
         }
       }
     }
+    if constexpr (k8) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-      if constexpr (k8) s[t] *= ksr[t];
+      for (int t = 0; t < 2; ++t) {
+        if constexpr (kLook != kInPage) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) ksr[t][v] = __shfl(ks_own[t], 4 * h + v);
+        }
+        s[t] *= ksr[t];
+      }
+    }
     load_k(next);
     __builtin_amdgcn_sched_barrier(0);
     // ---- keys that do not exist ----
@@ -559,6 +572,14 @@ kernel(Args a) {
       l_run += p[e];
     }
     if constexpr (k8) {
+      if constexpr (kLook != kInPage) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const float own = now.count[t] != 0 ? vs_own[t] : 0.f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) vsr[t][v] = __shfl(own, 4 * h + v);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] *= vsr[e >> 2][e & 3];
     }
@@ -653,13 +674,9 @@ kernel(Args a) {
 
 template <class E, class C, Look kLook>
 void launch_look(const Args &a, unsigned workgroups, hipStream_t stream) {
-  if constexpr (kLook == kElements) {
-    kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
-  } else {
-    if (a.d <= 64) kernel<E, C, 64, kLook><<<workgroups, kThreads, 0, stream>>>(a);
-    else if (a.d <= 128) kernel<E, C, 128, kLook><<<workgroups, kThreads, 0, stream>>>(a);
-    else kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
-  }
+  if (a.d <= 64) kernel<E, C, 64, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+  else if (a.d <= 128) kernel<E, C, 128, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+  else kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
 }
 template <class E, class C> void launch_cache(const Args &a, unsigned workgroups, hipStream_t stream) {
   // whole 16-byte chunks of a row, 8 bytes at its end in an 8-bit cache

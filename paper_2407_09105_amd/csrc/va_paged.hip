@@ -36,6 +36,14 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
   const int first = of.x, parts = of.y;
   if (parts == 1) return;  // its only workgroup has written the result
   const float2 *const ml = ws.ml + (size_t)first * hq + head;
+  const int c = t % kCols, x1 = t / kCols;  // this thread's column and first part
+  const float *const o = ws.o + ((size_t)first * hq + head) * d + min(c, d - 1);
+  float v[kFly];
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int k = 0; k < kFly; ++k) v[k] = o[(size_t)min(x0 + k * kJoinRows, parts - 1) * hq * d];
+  };
+  load(x1);  // on their way before the weights are known
   float2 mine[(kMostParts + kThreads - 1) / kThreads];
   float top = -INFINITY;
 #pragma unroll
@@ -62,16 +70,12 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
   if (t % 64 == 0) some[1][t / 64] = sum;
   __syncthreads();
   sum = some[1][0] + some[1][1] + some[1][2] + some[1][3];
-  const int c = t % kCols;
-  const float *const o = ws.o + ((size_t)first * hq + head) * d + min(c, d - 1);
   float y = 0.f;
-  for (int x0 = t / kCols; x0 < parts; x0 += kJoinRows * kFly) {
-    float v[kFly];
-#pragma unroll
-    for (int k = 0; k < kFly; ++k) v[k] = o[(size_t)min(x0 + k * kJoinRows, parts - 1) * hq * d];
+  for (int x0 = x1; x0 < parts; x0 += kJoinRows * kFly) {
 #pragma unroll
     for (int k = 0; k < kFly; ++k)
       if (x0 + k * kJoinRows < parts) y += weight[x0 + k * kJoinRows] * v[k];
+    load(x0 + kJoinRows * kFly);
   }
   if constexpr (kJoinRows > 1) {
     __syncthreads();  // both of `some` are read
