@@ -181,10 +181,12 @@ template <> struct shift_log2<F16> { static constexpr float value = 6.f; };
 
 // ---- the kernel ---------------------------------------------------------------------------------------
 
-// How a tile's rows are found: kInPage: page_size is a multiple of 16, and the 16 keys of a product lie next to each other; kPerKey:
-// each key on its own; kElements: likewise, and rows are read in dwords or single elements (head dims or addresses that 16-byte
-// chunks do not fit).
-enum Look { kInPage, kPerKey, kElements };
+// How a tile's rows are found and read.
+//   kWholeRows: page_size is a multiple of 16, so that the 16 keys of a product lie next to each other, and head_dim is kDh itself
+//   kInPage:    the pages likewise, any head_dim that 16-byte chunks fit
+//   kPerKey:    each key is found on its own
+//   kElements:  likewise, and rows are read in dwords or single elements (head dims or addresses that 16-byte chunks do not fit)
+enum Look { kWholeRows, kInPage, kPerKey, kElements };
 
 struct Args {
   const void *Q;
@@ -201,20 +203,50 @@ struct Args {
   float scale_log2;
 };
 
+// Between lanes 8 apart in a row of 16 (i and i + 8): before, lane l holds a of row l % 8 and b of row 8 + l % 8; after, the lower
+// lane both a's of its row, its own and the upper one's, and the upper lane both b's, the lower one's first.
+__device__ __forceinline__ void own_row(uint32_t &a, uint32_t &b) {
+  constexpr int kRotateBy8 = 0x128;
+  const int x = __builtin_amdgcn_update_dpp((int)a, (int)b, kRotateBy8, 0xf, 0xc, false);  // upper lanes: b of the lower
+  b = (uint32_t)__builtin_amdgcn_update_dpp((int)b, (int)a, kRotateBy8, 0xf, 0x3, false);  // lower lanes: a of the upper
+  a = (uint32_t)x;
+}
+// a = b = x of this lane's i -> a of i % 8, b of 8 + i % 8
+__device__ __forceinline__ void other_half(int &a, int &b) {
+  const int x = a;
+  a = __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xc, false);
+  b = __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0x3, false);
+}
+
+// What the lanes know of the 16 keys of a product, lane (i, h) of key i; turned: of key (i + 4 h) % 16; four_of: a turned value of
+// key 4 h + kV, which in each row of 16 lanes is lane kV's.
+__device__ __forceinline__ int turned(int x) {
+  const int lane = threadIdx.x & 63;
+  return __shfl(x, (lane + (lane >> 4) * 4) & 15);
+}
+template <int kV> __device__ __forceinline__ int four_of(int turned_x) {
+  return __builtin_amdgcn_update_dpp(turned_x, turned_x, 0x150 + kV, 0xf, 0xf, false);
+}
+__device__ __forceinline__ void four_of(float turned_x, f32x4 &y) {
+  const int x = (int)__float_as_uint(turned_x);
+  y = f32x4{__uint_as_float((uint32_t)four_of<0>(x)), __uint_as_float((uint32_t)four_of<1>(x)), __uint_as_float((uint32_t)four_of<2>(x)),
+            __uint_as_float((uint32_t)four_of<3>(x))};
+}
+
 template <int kBytes> struct Piece {
   uint32_t x[kBytes / 4];
 };
-template <int kBytes> __device__ __forceinline__ Piece<kBytes> buffer_piece(buffer_t b, uint32_t off) {
+template <int kBytes, int kPolicy> __device__ __forceinline__ Piece<kBytes> buffer_piece(buffer_t b, uint32_t off) {
   Piece<kBytes> p;
   if constexpr (kBytes == 16) {
-    const u32x4 r = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, 0);
+    const u32x4 r = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, kPolicy);
 #pragma unroll
     for (int i = 0; i < 4; ++i) p.x[i] = r[i];
   } else if constexpr (kBytes == 8) {
-    const u32x2 r = __builtin_amdgcn_raw_buffer_load_b64(b, (int)off, 0, 0);
+    const u32x2 r = __builtin_amdgcn_raw_buffer_load_b64(b, (int)off, 0, kPolicy);
     p.x[0] = r[0], p.x[1] = r[1];
   } else {
-    p.x[0] = __builtin_amdgcn_raw_buffer_load_b32(b, (int)off, 0, 0);
+    p.x[0] = __builtin_amdgcn_raw_buffer_load_b32(b, (int)off, 0, kPolicy);
   }
   return p;
 }
@@ -258,7 +290,7 @@ template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_
 template <class E, class C, int kDh, Look kLook>
 __global__ void __launch_bounds__(kThreads, is_f32<E>::value ? (kDh == 256 ? 1 : 2) : kDh == 256 ? 2 : 3)
 kernel(Args a) {
-  constexpr bool kF32 = is_f32<E>::value, k8 = is_8bit<C>::value;
+  constexpr bool kF32 = is_f32<E>::value, k8 = is_8bit<C>::value, kTogether = kLook <= kInPage;  // a product's keys
   typedef typename E::elem elem;
   typedef typename C::elem cached;
   constexpr int kSize = sizeof(cached);
@@ -279,7 +311,7 @@ kernel(Args a) {
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), i = lane & 15, h = lane >> 4;
   const PageMap &map = a.map;
-  const int hkv = map.hkv, d = a.d, G = a.G, page = map.page.d;
+  const int hkv = map.hkv, d = kLook == kWholeRows ? kDh : a.d, G = a.G, page = map.page.d;
 
   // Workgroup ids go to the 8 XCDs in turn: the groups of 16 query heads of one KV head, which read the same keys, 8 ids apart.
   const int turn = blockIdx.x >> 3, pair = turn / a.groups * 8 + (blockIdx.x & 7), head0 = turn % a.groups * kHeads;
@@ -331,17 +363,17 @@ kernel(Args a) {
 
   // ---- rows of a tile: the entries are requested two tiles ahead, the rows one ----
   struct Entries {
-    int j[2], at[2], id[2];  // key (kInPage: the product's first, else this lane's own), the page's place in the table, the page
+    int j[2], at[2], id[2];  // key (kTogether: the product's first, else this lane's own), the page's place in the table, the page
   };
   struct Rows {
-    int row[2];    // of that key; row 0 where it does not exist (kInPage: not read then)
-    int count[2];  // keys that exist, kInPage: of the product's 16, else of this lane's one
+    int row[2];    // of that key; row 0 where it does not exist (kTogether: not read then)
+    int count[2];  // kTogether: how many of the product's 16 keys exist; else which, a bit each
   };
   auto entries = [&](int tile) {
     Entries t;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      t.j[s] = tile * kTile + 16 * s + (kLook == kInPage ? 0 : i);
+      t.j[s] = tile * kTile + 16 * s + (kTogether ? 0 : i);
       t.at[s] = min(t.j[s], j1 - 1) / map.page;
       t.id[s] = table[t.at[s]];
     }
@@ -353,18 +385,28 @@ kernel(Args a) {
     for (int s = 0; s < 2; ++s) {
       const bool ok = t.j[s] < j1 && (uint32_t)t.id[s] < (uint32_t)map.n_pages;
       r.row[s] = ok ? (t.id[s] * hkv + g) * page + (t.j[s] - t.at[s] * page) : 0;
-      r.count[s] = !ok ? 0 : kLook == kInPage ? min(j1 - t.j[s], 16) : 1;
+      if constexpr (kTogether) r.count[s] = ok ? min(j1 - t.j[s], 16) : 0;
+      else r.count[s] = (int)((uint32_t)__ballot(ok) & 0xffffu);  // the four groups of 16 lanes have the same keys
     }
     return r;
   };
 
   const uint32_t row_bytes = (uint32_t)d * kSize;
-  uint32_t k_off[kKn], v_off[kHf];  // column offsets in a row, kPastEnd for columns that do not exist
+  // A load of K takes whole 128-byte lines: chunks 8 x .. 8 x + 7 of rows 0..7 (a) or 8..15 (b), lane (i, h) chunk 4 (i / 8) + h of
+  // row i % 8.  The lanes 8 apart then swap what is the other's row (own_row), and hold chunks 4 n + h, n = 2 x and 2 x + 1, of
+  // their own row i.  Rows of 64 bytes have 4 chunks: a load takes the 16 rows as they are.
+  constexpr bool kLines = kKn > 1;
+  constexpr int kLoads = kLines ? kKn / 2 : 1;  // of one kind
+  const int k_row = kLines ? i & 7 : i, k_chunk = kLines ? 4 * (i >> 3) + h : h;
+  uint32_t k_off[kLoads], v_off[kHf];  // column offsets in a row, kPastEnd for columns that do not exist
 #pragma unroll
-  for (int x = 0; x < kKn; ++x) k_off[x] = (4 * x + h) * kCpc < d ? (uint32_t)(i * row_bytes + (4 * x + h) * 16) : kPastEnd;
+  for (int x = 0; x < kLoads; ++x) k_off[x] = (8 * x + k_chunk) * kCpc < d ? (uint32_t)(k_row * row_bytes + (8 * x + k_chunk) * 16) : kPastEnd;
 #pragma unroll
   for (int x = 0; x < kHf; ++x) v_off[x] = (16 * x + i) * kVC < d ? (uint32_t)(4 * h * row_bytes + (16 * x + i) * kVBytes) : kPastEnd;
   const bool half_chunk = k8 && (d & 8) != 0;  // rows end in the middle of a 16-byte chunk
+  // Rows are read once and pass by the caches' other contents (non-temporal loads) where a load takes whole 128-byte lines: this card
+  // reads 7.0 TB/s so, 6.1 otherwise.  A line fetched in pieces would be fetched again: with rows of 160 bytes 250 us became 266.
+  constexpr int kPolicyK = kLook == kWholeRows ? kOnce : 0, kPolicyV = kDh * kSize >= 128 ? kOnce : 0;
 
   const bool dwords = kLook == kElements && (row_bytes & 3) == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0;
 
@@ -372,95 +414,84 @@ kernel(Args a) {
   typedef Piece<kVBytes> VPiece;
   KPiece kr[2][kKn];
   VPiece vr[8][kHf];
-  // scales: kInPage of keys 4 h + 0..3; else of this lane's key, handed round when they are used
+  // scales: kTogether of keys 4 h + 0..3; else of key (i + 4 h) % 16, handed round (four_of) when they are used
   f32x4 ksr[2], vsr[2];
-  float ks_own[2], vs_own[2];
+  float ks_turned[2], vs_turned[2];
 
   auto load_k = [&](const Rows &r) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if constexpr (kLook == kInPage) {
+      if constexpr (kTogether) {
         const buffer_t buf = make_buffer((const char *)a.k + (size_t)r.row[s] * row_bytes, (size_t)r.count[s] * row_bytes);
-        if (!half_chunk) {
 #pragma unroll
-          for (int x = 0; x < kKn; ++x) kr[s][x] = buffer_piece<16>(buf, k_off[x]);
-        } else {
-#pragma unroll
-          for (int x = 0; x < kKn; ++x) {
-            const Piece<8> lo = buffer_piece<8>(buf, k_off[x]);
-            const Piece<8> hi = buffer_piece<8>(buf, (4 * x + h) * kCpc + 8 < d ? k_off[x] + 8 : kPastEnd);
+        for (int x = 0; x < kKn; ++x) {  // a, b, a, b, ...
+          const uint32_t base = k_off[x / 2], off = base == kPastEnd ? kPastEnd : base + (x % 2) * 8 * row_bytes;
+          if (!half_chunk) {
+            kr[s][x] = buffer_piece<16, kPolicyK>(buf, off);
+          } else {
+            const Piece<8> lo = buffer_piece<8, 0>(buf, off);
+            const Piece<8> hi = buffer_piece<8, 0>(buf, (8 * (x / 2) + k_chunk) * kCpc + 8 < d ? off + 8 : kPastEnd);
             kr[s][x] = {{lo.x[0], lo.x[1], hi.x[0], hi.x[1]}};
           }
         }
         if constexpr (k8) {
           const buffer_t sb = make_buffer(a.ks + r.row[s], r.count[s] > 0 ? 64 : 0);
-          const Piece<16> y = buffer_piece<16>(sb, 16 * h);
+          const Piece<16> y = buffer_piece<16, 0>(sb, 16 * h);
 #pragma unroll
           for (int v = 0; v < 4; ++v) ksr[s][v] = __uint_as_float(y.x[v]);
         }
       } else {
-        const char *row = (const char *)a.k + (size_t)r.row[s] * row_bytes;  // row 0 for a key that does not exist
-        if constexpr (kLook == kElements) {
+        // rows of the two kinds of loads; row 0 for a key that does not exist
+        int from[2] = {r.row[s], r.row[s]};
+        if constexpr (kLines) other_half(from[0], from[1]);
 #pragma unroll
-          for (int x = 0; x < kKn; ++x) kr[s][x] = element_piece<cached, 16>((const cached *)row, (4 * x + h) * kCpc, d, dwords);
-        } else if (d == kDh) {
-#pragma unroll
-          for (int x = 0; x < kKn; ++x) kr[s][x] = memory_piece<16>(row + (4 * x + h) * 16);
-        } else {
-#pragma unroll
-          for (int x = 0; x < kKn; ++x) {
-            const int column = (4 * x + h) * kCpc;
-            kr[s][x] = {};
-            if (column + kCpc <= d) {
-              kr[s][x] = memory_piece<16>(row + column * kSize);
-            } else if (half_chunk && column < d) {
-              const Piece<8> lo = memory_piece<8>(row + column * kSize);
-              kr[s][x].x[0] = lo.x[0], kr[s][x].x[1] = lo.x[1];
-            }
+        for (int x = 0; x < kKn; ++x) {
+          const char *row = (const char *)a.k + (size_t)from[x % 2] * row_bytes;
+          const int column = (8 * (x / 2) + k_chunk) * kCpc;
+          // (columns that do not exist are loaded from the row's end; what is not q's to see is cleared before it is used)
+          if constexpr (kLook == kElements) {
+            kr[s][x] = element_piece<cached, 16>((const cached *)row, column, d, dwords);
+          } else if (!half_chunk) {
+            kr[s][x] = memory_piece<16>(row + min(column, d - kCpc) * kSize);
+          } else {
+            const Piece<8> lo = memory_piece<8>(row + min(column, d - 8) * kSize), hi = memory_piece<8>(row + min(column + 8, d - 8) * kSize);
+            kr[s][x] = {{lo.x[0], lo.x[1], hi.x[0], hi.x[1]}};
           }
         }
-        if constexpr (k8) ks_own[s] = a.ks[r.row[s]];
+        if constexpr (k8) ks_turned[s] = a.ks[turned(r.row[s])];
       }
     }
   };
   auto load_v = [&](const Rows &r) {
-    const bool all = kLook == kPerKey && d == 16 * kVC * kHf && !__any(r.count[0] == 0 || r.count[1] == 0);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if constexpr (kLook == kInPage) {
+      if constexpr (kTogether) {
         const buffer_t buf = make_buffer((const char *)a.v + (size_t)r.row[s] * row_bytes, (size_t)r.count[s] * row_bytes);
 #pragma unroll
         for (int v = 0; v < 4; ++v)
 #pragma unroll
-          for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = buffer_piece<kVBytes>(buf, v_off[x] == kPastEnd ? kPastEnd : v_off[x] + v * row_bytes);
+          for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = buffer_piece<kVBytes, kPolicyV>(buf, v_off[x] == kPastEnd ? kPastEnd : v_off[x] + v * row_bytes);
         if constexpr (k8) {
           const buffer_t sb = make_buffer(a.vs + r.row[s], r.count[s] > 0 ? 64 : 0);
-          const Piece<16> y = buffer_piece<16>(sb, 16 * h);
+          const Piece<16> y = buffer_piece<16, 0>(sb, 16 * h);
 #pragma unroll
           for (int v = 0; v < 4; ++v) vsr[s][v] = __uint_as_float(y.x[v]);
         }
       } else {
+        const int turned_row = turned(r.row[s]);
+        const int from[4] = {four_of<0>(turned_row), four_of<1>(turned_row), four_of<2>(turned_row), four_of<3>(turned_row)};
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const int from = __shfl(r.row[s], 4 * h + v);
-          const bool ok = __shfl(r.count[s], 4 * h + v) != 0;
-          const char *row = (const char *)a.v + (size_t)from * row_bytes;
-          if constexpr (kLook == kElements) {
+          const char *row = (const char *)a.v + (size_t)from[v] * row_bytes;
 #pragma unroll
-            for (int x = 0; x < kHf; ++x)
-              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, ok ? d : 0, dwords);
-          } else if (all) {
-#pragma unroll
-            for (int x = 0; x < kHf; ++x) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
-          } else {
-#pragma unroll
-            for (int x = 0; x < kHf; ++x) {
-              vr[4 * s + v][x] = {};
-              if (ok && (16 * x + i) * kVC < d) vr[4 * s + v][x] = memory_piece<kVBytes>(row + (16 * x + i) * kVBytes);
-            }
+          for (int x = 0; x < kHf; ++x) {
+            if constexpr (kLook == kElements)
+              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, d, dwords);
+            else
+              vr[4 * s + v][x] = memory_piece<kVBytes>(row + min((16 * x + i) * kVC, d - kVC) * kSize);
           }
         }
-        if constexpr (k8) vs_own[s] = a.vs[r.row[s]];
+        if constexpr (k8) vs_turned[s] = a.vs[turned_row];
       }
     }
   };
@@ -490,6 +521,24 @@ kernel(Args a) {
     __builtin_amdgcn_sched_barrier(0);  // they are on their way before the keys are waited for
     // ---- S^T = K Q^T ----
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if constexpr (kLines) {
+#pragma unroll
+      for (int x = 0; x < kKn; x += 2)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) own_row(kr[t][x].x[w], kr[t][x + 1].x[w]);
+    }
+    if constexpr (kLook == kPerKey) {
+      if (d != kDh) {
+#pragma unroll
+        for (int x = 0; x < kKn; ++x)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) kr[t][x].x[w] = (4 * x + h) * kCpc + w * 4 / kSize < d ? kr[t][x].x[w] : 0u;
+      }
+    }
 #pragma unroll
     for (int x = 0; x < kKn; ++x) {
 #pragma unroll
@@ -522,17 +571,14 @@ kernel(Args a) {
     if constexpr (k8) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if constexpr (kLook != kInPage) {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) ksr[t][v] = __shfl(ks_own[t], 4 * h + v);
-        }
+        if constexpr (!kTogether) four_of(ks_turned[t], ksr[t]);
         s[t] *= ksr[t];
       }
     }
     load_k(next);
     __builtin_amdgcn_sched_barrier(0);
     // ---- keys that do not exist ----
-    if constexpr (kLook == kInPage) {
+    if constexpr (kTogether) {
       if (now.count[0] + now.count[1] < kTile) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -544,11 +590,20 @@ kernel(Args a) {
           }
       }
     } else {
+      if (now.count[0] != 0xffff || now.count[1] != 0xffff) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint32_t there = (uint32_t)__ballot(now.count[t] != 0) & 0xffffu;
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t mine = (uint32_t)now.count[t] >> (4 * h);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) s[t][v] = there >> (4 * h + v) & 1 ? s[t][v] : -INFINITY;
+          for (int v = 0; v < 4; ++v) {
+            const bool there = mine >> v & 1;
+            s[t][v] = there ? s[t][v] : -INFINITY;
+#pragma unroll
+            for (int x = 0; x < kHf; ++x)  // row 0 was read instead
+#pragma unroll
+              for (int w = 0; w < kVBytes / 4; ++w) vr[4 * t + v][x].x[w] = there ? vr[4 * t + v][x].x[w] : 0u;
+          }
+        }
       }
     }
     // ---- softmax ----
@@ -572,12 +627,12 @@ kernel(Args a) {
       l_run += p[e];
     }
     if constexpr (k8) {
-      if constexpr (kLook != kInPage) {
+      if constexpr (!kTogether) {
+        four_of(vs_turned[0], vsr[0]);
+        four_of(vs_turned[1], vsr[1]);
+        if (now.count[0] != 0xffff || now.count[1] != 0xffff) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float own = now.count[t] != 0 ? vs_own[t] : 0.f;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) vsr[t][v] = __shfl(own, 4 * h + v);
+          for (int e = 0; e < 8; ++e) vsr[e >> 2][e & 3] = (uint32_t)now.count[e >> 2] >> (4 * h + (e & 3)) & 1 ? vsr[e >> 2][e & 3] : 0.f;
         }
       }
 #pragma unroll
@@ -674,7 +729,7 @@ kernel(Args a) {
 
 template <class E, class C, Look kLook>
 void launch_look(const Args &a, unsigned workgroups, hipStream_t stream) {
-  if (a.d <= 64) kernel<E, C, 64, kLook><<<workgroups, kThreads, 0, stream>>>(a);
+  if (kLook != kWholeRows ? a.d <= 64 : a.d == 64) kernel<E, C, 64, kLook><<<workgroups, kThreads, 0, stream>>>(a);
   else if (a.d <= 128) kernel<E, C, 128, kLook><<<workgroups, kThreads, 0, stream>>>(a);
   else kernel<E, C, 256, kLook><<<workgroups, kThreads, 0, stream>>>(a);
 }
@@ -683,6 +738,7 @@ template <class E, class C> void launch_cache(const Args &a, unsigned workgroups
   constexpr int kSize = sizeof(typename C::elem), kEven = is_8bit<C>::value ? 8 : 16 / kSize;
   const bool chunks = a.d % kEven == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & (kEven * kSize - 1)) == 0 && ((uintptr_t)a.Q & 3) == 0;
   if (!chunks) launch_look<E, C, kElements>(a, workgroups, stream);
+  else if (a.map.page.d % 16 == 0 && (a.d == 64 || a.d == 128 || a.d == 256)) launch_look<E, C, kWholeRows>(a, workgroups, stream);
   else if (a.map.page.d % 16 == 0) launch_look<E, C, kInPage>(a, workgroups, stream);
   else launch_look<E, C, kPerKey>(a, workgroups, stream);
 }

@@ -7,14 +7,17 @@
 namespace va {
 namespace paged {
 
-// Workgroups that the parts should make where the lengths allow it: 256 CUs hold 768.
+// Workgroups that the cuts should add, where the lengths allow it, to the one that every sequence has for each KV head: 256 CUs hold
+// 768, and up to twice as many even out what sequences of different lengths leave.
 constexpr int kWorkgroups = 1024;
 constexpr int kLeastUnits = 2;
+constexpr int kFewParts = 8;
 
 Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
   const int groups = ceil_div(hq / hkv, kHeads);
   const long long least = kLeastUnits * kUnit, most = n_seqs * ((capacity + least - 1) / least);  // parts that there can be
-  const long long room = (kWorkgroups + (long long)hkv * groups - 1) / ((long long)hkv * groups);
+  const long long each = (long long)hkv * groups, more = std::min<long long>(kWorkgroups, n_seqs * each);
+  const long long room = (kWorkgroups + more + each - 1) / each;
   if (capacity <= least) return {n_seqs, kLeastUnits, fast_div(1)};
   const int extra = (int)std::min(room, most);
   return {n_seqs + extra, kLeastUnits, fast_div(extra)};
@@ -24,7 +27,7 @@ namespace {
 
 // One workgroup per (sequence, query head) adds up the parts' sums, weighted relative to the largest reference exponent: every
 // kJoinRows-th part one group of threads', a column each, and then the groups' sums in order.
-constexpr int kMostParts = kWorkgroups + 1;  // of one sequence
+constexpr int kMostParts = 2 * kWorkgroups + 1;  // of one sequence
 
 template <class E, int kCols>  // kCols: threads of a group, d rounded up to 64, 128 or 256
 __global__ void __launch_bounds__(kThreads)
@@ -89,9 +92,63 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
   if (t == 0) LSE[(size_t)head * n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
-template <class E> void launch_join(void *O, float *LSE, const Workspace &ws, int n_seqs, int hq, int d, hipStream_t stream) {
+// The same by one wave per (sequence, query head), four of them in a workgroup, for batches in which a sequence has few parts: a
+// column per lane and 64 of d, the weights of 64 parts at a time in the lanes.
+template <class E, int kCols>
+__global__ void __launch_bounds__(kThreads)
+join_few_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d) {
+  constexpr int kOwn = kCols / 64, kFly = 4;
+  const int b = blockIdx.x, head = blockIdx.y * kWaves + uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (head >= hq) return;
+  const int2 of = ws.parts[b];
+  const int first = uniform(of.x), parts = uniform(of.y);
+  if (parts == 1) return;
+  const float2 *const ml = ws.ml + (size_t)first * hq + head;
+  const float *const o = ws.o + ((size_t)first * hq + head) * d;
+  float top = -INFINITY;
+  for (int x = lane; x < parts; x += 64) top = fmaxf(top, ml[(size_t)x * hq].x);
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+  float sum = 0.f, y[kOwn] = {};
+  for (int x0 = 0; x0 < parts; x0 += 64) {
+    const int x = x0 + lane;
+    const float2 one = x < parts ? ml[(size_t)x * hq] : make_float2(-INFINITY, 0.f);
+    const float weight = one.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(one.x - top);
+    sum += weight * one.y;
+    const int many = min(parts - x0, 64);
+    for (int k0 = 0; k0 < many; k0 += kFly) {
+      float v[kFly][kOwn];
+#pragma unroll
+      for (int k = 0; k < kFly; ++k)
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) v[k][e] = o[(size_t)(x0 + min(k0 + k, many - 1)) * hq * d + min(lane + 64 * e, d - 1)];
+#pragma unroll
+      for (int k = 0; k < kFly; ++k) {
+        if (k0 + k >= many) continue;
+        const float w = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), k0 + k));
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) y[e] += w * v[k][e];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e)
+    if (lane + 64 * e < d) O[((size_t)b * hq + head) * d + lane + 64 * e] = (typename E::elem)(sum != 0.f ? y[e] / sum : 0.f);
+  if (lane == 0) LSE[(size_t)head * n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <class E> void launch_join(void *O, float *LSE, const Workspace &ws, const Split &split, int n_seqs, int hq, int d, hipStream_t stream) {
   const dim3 grid((unsigned)n_seqs, (unsigned)hq);
   typename E::elem *const o = (typename E::elem *)O;
+  if ((int)split.extra.d <= kFewParts * n_seqs) {
+    const dim3 few((unsigned)n_seqs, (unsigned)ceil_div(hq, kWaves));
+    if (d <= 64) join_few_kernel<E, 64><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+    else if (d <= 128) join_few_kernel<E, 128><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+    else join_few_kernel<E, 256><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+    return;
+  }
   if (d <= 64) join_kernel<E, 64><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
   else if (d <= 128) join_kernel<E, 128><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
   else join_kernel<E, 256><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
@@ -117,7 +174,7 @@ hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const v
   (dt == VA_BF16 ? launch_bf16 : dt == VA_F16 ? launch_f16 : launch_f32)(a, c.format, (unsigned)workgroups, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || split.slots == c.n_seqs) return e;
-  (dt == VA_BF16 ? launch_join<Bf16> : dt == VA_F16 ? launch_join<F16> : launch_join<F32>)(O, LSE, ws, c.n_seqs, hq, c.d, stream);
+  (dt == VA_BF16 ? launch_join<Bf16> : dt == VA_F16 ? launch_join<F16> : launch_join<F32>)(O, LSE, ws, split, c.n_seqs, hq, c.d, stream);
   return hipGetLastError();
 }
 
