@@ -20,19 +20,26 @@ __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) 
   return it == VA_I64 ? (long long)((const int64_t *)ids)[t] : (long long)((const int32_t *)ids)[t];
 }
 
-// kLanes lanes hold a row, lane l its elements l * kVec .. + kVec - 1 (kStep = 1) or l, l + kLanes, ... (kVec = 1).
-template <class E, class C, int kVec, int kLanes>
+// kLanes lanes hold a row, lane l its elements l * kVec .. + kVec - 1, or l, l + kLanes, ... (kVec = 1).  kWhole: d is kVec * kLanes.
+// Stores of whole 128-byte lines pass by the caches (non-temporal; lines that two rows share would be written twice): 65536 tokens
+// of 8 heads of 128 written behind a rotary embedding of K 152 -> 128 us, read back 211 -> 193, and 2 to 3 % slower to 8 % faster
+// together with the next reader of the rows.  Loads do not: the rows to be written have often just left another kernel (16384 of
+// those tokens behind the embedding 35 us, with such loads 38).
+template <class E, class C, int kVec, int kLanes, bool kWhole>
 struct Row {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
   static constexpr int kPer = kVec > 1 ? kVec : 256 / kLanes;   // elements of a lane
+  template <class T> static constexpr bool kPast = kWhole && sizeof(T) * kVec * kLanes % 128 == 0;
+  template <class T> using Words = uint32_t __attribute__((ext_vector_type(sizeof(T) * kVec / 4)));
   static __device__ __forceinline__ int column(int lane, int e) { return kVec > 1 ? lane * kVec + e : lane + e * kLanes; }
 
   template <class T> static __device__ __forceinline__ void load(const T *p, int lane, int d, T (&x)[kPer]) {
     if constexpr (kVec > 1) {
-      struct __attribute__((aligned(sizeof(T) * kVec))) Chunk { T x[kVec]; };
-      if (lane * kVec < d) {
-        const Chunk c = *(const Chunk *)(p + lane * kVec);
+      struct Chunk { T x[kVec]; };
+      if (kWhole || lane * kVec < d) {
+        const Words<T> *const at = (const Words<T> *)(p + lane * kVec);
+        const Chunk c = __builtin_bit_cast(Chunk, *at);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) x[e] = c.x[e];
       } else {
@@ -46,12 +53,13 @@ struct Row {
   }
   template <class T> static __device__ __forceinline__ void store(T *p, int lane, int d, const T (&x)[kPer]) {
     if constexpr (kVec > 1) {
-      struct __attribute__((aligned(sizeof(T) * kVec))) Chunk { T x[kVec]; };
-      if (lane * kVec < d) {
-        Chunk c;
+      struct Chunk { T x[kVec]; } c;
+      if (kWhole || lane * kVec < d) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) c.x[e] = x[e];
-        *(Chunk *)(p + lane * kVec) = c;
+        Words<T> *const at = (Words<T> *)(p + lane * kVec);
+        if (kPast<T>) __builtin_nontemporal_store(__builtin_bit_cast(Words<T>, c), at);
+        else *at = __builtin_bit_cast(Words<T>, c);
       }
     } else {
 #pragma unroll
@@ -85,68 +93,105 @@ struct Row {
   }
 };
 
-// One row of K and of V per kLanes lanes; workgroup: kThreads / kLanes consecutive tokens of one head.
-template <class E, class C, int kVec, int kLanes>
+// kItems rows of K and of V per kLanes lanes, their loads and look-ups in flight together; workgroup: kItems * kThreads / kLanes
+// consecutive tokens of one head.
+template <class C> constexpr int items() { return is_8bit<C>::value ? 2 : 1; }
+
+template <int kLanes, int kItems> struct Tokens {
+  int t[kItems];
+  bool there[kItems];
+  __device__ __forceinline__ Tokens(long long group, int N) {
+    constexpr int kRows = kThreads / kLanes;
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const long long at = (group * kItems + u) * kRows + threadIdx.x / kLanes;
+      there[u] = at < N;
+      t[u] = there[u] ? (int)at : N - 1;
+    }
+  }
+};
+
+template <class E, class C, int kVec, int kLanes, bool kWhole>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
-             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, int H, int d) {
-  typedef Row<E, C, kVec, kLanes> R;
-  const int lane = threadIdx.x % kLanes, g = blockIdx.x % H;
-  const long long t = (long long)(blockIdx.x / H) * (kThreads / kLanes) + threadIdx.x / kLanes;
-  if (t >= N) return;
-  const int place = place_of(map, seq_ids ? seq_ids[t] : t, id_at(pos, it, (int)t));
-  if (place < 0) return;
-  const size_t row = (size_t)place + (size_t)g * map.page.d, from = ((size_t)t * H + g) * d;
-  typename E::elem k[R::kPer], v[R::kPer];
-  R::load(K + from, lane, d, k);
-  R::load(V + from, lane, d, v);
-  if constexpr (is_8bit<C>::value) {
-    typename C::elem q[R::kPer];
-    const float sk = R::quantise(k, q);
-    R::store(Kc + row * d, lane, d, q);
-    const float sv = R::quantise(v, q);
-    R::store(Vc + row * d, lane, d, q);
-    if (lane == 0) {
-      ks[row] = sk;
-      vs[row] = sv;
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
+  typedef Row<E, C, kVec, kLanes, kWhole> R;
+  constexpr int kItems = items<C>();
+  const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
+  const Tokens<kLanes, kItems> tokens(group, N);
+  typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
+  int place[kItems];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const size_t from = ((size_t)tokens.t[u] * H + g) * d;
+    R::load(K + from, lane, d, k[u]);
+    R::load(V + from, lane, d, v[u]);
+    place[u] = place_of(map, seq_ids ? seq_ids[tokens.t[u]] : tokens.t[u], id_at(pos, it, tokens.t[u]));
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    if (!tokens.there[u] || place[u] < 0) continue;
+    const size_t row = (size_t)place[u] + (size_t)g * map.page.d;
+    if constexpr (is_8bit<C>::value) {
+      typename C::elem q[R::kPer];
+      const float sk = R::quantise(k[u], q);
+      R::store(Kc + row * d, lane, d, q);
+      const float sv = R::quantise(v[u], q);
+      R::store(Vc + row * d, lane, d, q);
+      if (lane == 0) {
+        ks[row] = sk;
+        vs[row] = sv;
+      }
+    } else {
+      R::store(Kc + row * d, lane, d, k[u]);
+      R::store(Vc + row * d, lane, d, v[u]);
     }
-  } else {
-    R::store(Kc + row * d, lane, d, k);
-    R::store(Vc + row * d, lane, d, v);
   }
 }
 
-template <class E, class C, int kVec, int kLanes>
+template <class E, class C, int kVec, int kLanes, bool kWhole>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
-            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, int H, int d) {
-  typedef Row<E, C, kVec, kLanes> R;
-  const int lane = threadIdx.x % kLanes, g = blockIdx.x % H;
-  const long long t = (long long)(blockIdx.x / H) * (kThreads / kLanes) + threadIdx.x / kLanes;
-  if (t >= N) return;
-  const int place = place_of(map, seq_ids ? seq_ids[t] : t, id_at(pos, it, (int)t));
-  const size_t row = (size_t)place + (size_t)g * map.page.d, to = ((size_t)t * H + g) * d;
-  typename E::elem k[R::kPer] = {}, v[R::kPer] = {};
-  if (place >= 0) {
-    if constexpr (is_8bit<C>::value) {
-      typename C::elem qk[R::kPer], qv[R::kPer];
-      R::load(Kc + row * d, lane, d, qk);
-      R::load(Vc + row * d, lane, d, qv);
-      const float sk = ks[row], sv = vs[row];
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
+  typedef Row<E, C, kVec, kLanes, kWhole> R;
+  constexpr int kItems = items<C>();
+  const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
+  const Tokens<kLanes, kItems> tokens(group, N);
+  typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
+  float sk[kItems], sv[kItems];
+  int place[kItems];
 #pragma unroll
-      for (int e = 0; e < R::kPer; ++e) {
-        k[e] = (typename E::elem)(cached_to_f32(C(), qk[e]) * sk);
-        v[e] = (typename E::elem)(cached_to_f32(C(), qv[e]) * sv);
-      }
-    } else {
-      R::load(Kc + row * d, lane, d, k);
-      R::load(Vc + row * d, lane, d, v);
-    }
+  for (int u = 0; u < kItems; ++u)
+    place[u] = place_of(map, seq_ids ? seq_ids[tokens.t[u]] : tokens.t[u], id_at(pos, it, tokens.t[u]));
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const size_t row = (size_t)max(place[u], 0) + (size_t)g * map.page.d;  // of page 0 where there is none
+    R::load(Kc + row * d, lane, d, k[u]);
+    R::load(Vc + row * d, lane, d, v[u]);
+    if constexpr (is_8bit<C>::value) sk[u] = ks[row], sv[u] = vs[row];
   }
-  R::store(K + to, lane, d, k);
-  R::store(V + to, lane, d, v);
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    if (!tokens.there[u]) continue;
+    typename E::elem x[R::kPer], y[R::kPer];
+#pragma unroll
+    for (int e = 0; e < R::kPer; ++e) {
+      x[e] = y[e] = (typename E::elem)0.f;
+      if (place[u] >= 0) {
+        if constexpr (is_8bit<C>::value) {
+          x[e] = (typename E::elem)(cached_to_f32(C(), k[u][e]) * sk[u]);
+          y[e] = (typename E::elem)(cached_to_f32(C(), v[u][e]) * sv[u]);
+        } else {
+          x[e] = k[u][e], y[e] = v[u][e];
+        }
+      }
+    }
+    const size_t to = ((size_t)tokens.t[u] * H + g) * d;
+    R::store(K + to, lane, d, x);
+    R::store(V + to, lane, d, y);
+  }
 }
 
 struct Call {
@@ -160,22 +205,27 @@ struct Call {
   hipStream_t stream;
 };
 
-template <class E, class C, int kVec, int kLanes> hipError_t launch(const Call &a) {
+template <class E, class C, int kVec, int kLanes, bool kWhole> hipError_t launch_rows(const Call &a) {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
-  constexpr int kTokens = kThreads / kLanes;
+  constexpr int kTokens = kThreads / kLanes * items<C>();
   const long long groups = ((long long)a.N + kTokens - 1) / kTokens * a.c.hkv;
   if (groups > 0x7fffffffll) return hipErrorInvalidValue;
   const PageMap map = page_map(a.c);
+  const FastDiv heads = fast_div(a.c.hkv);
   if (a.write)
-    write_kernel<E, C, kVec, kLanes><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+    write_kernel<E, C, kVec, kLanes, kWhole><<<(unsigned)groups, kThreads, 0, a.stream>>>(
         (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-        a.N, a.c.hkv, a.c.d);
+        a.N, heads, a.c.d);
   else
-    read_kernel<E, C, kVec, kLanes><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+    read_kernel<E, C, kVec, kLanes, kWhole><<<(unsigned)groups, kThreads, 0, a.stream>>>(
         (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-        a.N, a.c.hkv, a.c.d);
+        a.N, heads, a.c.d);
   return hipGetLastError();
+}
+
+template <class E, class C, int kVec, int kLanes> hipError_t launch(const Call &a) {
+  return kVec > 1 && a.c.d == kVec * kLanes ? launch_rows<E, C, kVec, kLanes, (kVec > 1)>(a) : launch_rows<E, C, kVec, kLanes, false>(a);
 }
 
 // Chunks of 16 bytes of K and V where the rows of both sides consist of whole aligned ones, else single elements.
@@ -187,7 +237,8 @@ template <class E, class C> hipError_t launch_ec(const Call &a) {
   if (chunks <= 8) return launch<E, C, kVec, 8>(a);
   if (chunks <= 16) return launch<E, C, kVec, 16>(a);
   if (chunks <= 32) return launch<E, C, kVec, 32>(a);
-  return launch<E, C, kVec, 64>(a);
+  if constexpr (kVec == 4) return launch<E, C, kVec, 64>(a);  // d <= 256
+  else return hipErrorInvalidValue;
 }
 template <class E> hipError_t launch_e(const Call &a) {
   if (a.c.format == VA_CACHE_I8) return launch_ec<E, I8>(a);
