@@ -301,7 +301,6 @@ kernel(Args a) {
   // matrix operands: of the queries' type, but P goes with 8-bit values as bf16, which has the range for their scales
   typedef typename std::conditional<kF32, Bf16, E>::type E16;
   typedef typename std::conditional<k8, Bf16, E16>::type P16;
-  typedef typename E16::x8 qx8;
   typedef typename P16::x8 px8;
   constexpr float kShift = kF32 ? 0.f : shift_log2<P16>::value;
 
@@ -323,37 +322,32 @@ kernel(Args a) {
   const int heads = min(G - head0, kHeads);  // rows of this workgroup
   const size_t first_head = (size_t)b * a.hq + g * G + head0;
 
-  // q as operand B: head i, the columns of the K chunks
-  constexpr int kQf = kF32 ? kKn * kCpc : kKn * kCpc / 8;
-  typename std::conditional<kF32, float, qx8>::type qf[kQf];
-  if constexpr (kLook == kElements) {
-    const elem *q = (const elem *)a.Q + (first_head + min(i, heads - 1)) * d;
-    auto q_at = [&](int column) { return i < heads && column < d ? q[min(column, d - 1)] : (elem)0.f; };
-#pragma unroll
-    for (int x = 0; x < kKn; ++x)
-#pragma unroll
-      for (int e = 0; e < kCpc; ++e) {
-        const elem y = q_at((4 * x + h) * kCpc + e);
-        if constexpr (kF32) qf[x * kCpc + e] = y;
-        else qf[(x * kCpc + e) / 8][e % 8] = y;
-      }
-  } else {
-    constexpr int kEach = 16 / (int)sizeof(elem);
+  // q as operand B, head i, the columns of the K chunks: kQn times 16 bytes a lane.  They stay in registers but where
+  // those do not suffice for two waves per SIMD, head_dim 256 of 16 or 32 bits: there every tile reads them from LDS anew (16 sequences
+  // of 500 to 4000 tokens, 16 heads: 114 us with spills, 107 with one wave, 107 so; scattered keys 120, 112, 107).
+  constexpr int kEach = 16 / (int)sizeof(elem), kQn = kKn * kCpc / kEach;
+  constexpr bool kQInLds = kDh == 256 && !k8;
+  __shared__ u32x4 q_lds[kQInLds ? kQn : 1][64];
+  u32x4 q_reg[kQn];
+  {
     const buffer_t q = make_buffer((const elem *)a.Q + first_head * d, (size_t)heads * d * sizeof(elem));  // no rows behind `heads`
 #pragma unroll
-    for (int x = 0; x < kKn; ++x)
-#pragma unroll
-      for (int e = 0; e < kCpc; e += kEach) {
-        const int column = (4 * x + h) * kCpc + e;
-        const u32x4 y = buffer_load16(q, column < d ? (uint32_t)((i * d + column) * sizeof(elem)) : kPastEnd);
-        if constexpr (kF32) {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) qf[x * kCpc + e + v] = __uint_as_float(y[v]);
-        } else {
-          qf[(x * kCpc + e) / 8] = as_x8<E16>(y);
-        }
+    for (int x = 0; x < kQn; ++x) {
+      const int column = (4 * (x * kEach / kCpc) + h) * kCpc + x * kEach % kCpc;
+      u32x4 y;
+      if constexpr (kLook == kElements) {
+        const Piece<16> piece = element_piece<elem, 16>((const elem *)a.Q + (first_head + min(i, heads - 1)) * d, column, i < heads ? d : 0, false);
+        y = u32x4{piece.x[0], piece.x[1], piece.x[2], piece.x[3]};
+      } else {
+        y = buffer_load16(q, column < d ? (uint32_t)((i * d + column) * sizeof(elem)) : kPastEnd);
       }
+      q_reg[x] = y;
+    }
   }
+  auto q_at = [&](int x) {
+    if constexpr (kQInLds) return q_lds[x][lane];
+    else return q_reg[x];
+  };
 
   // keys j0 .. j1 - 1, tiles wave, wave + kWaves, ...
   const long long j0l = (long long)(slot - part.first) * part.units * kUnit;
@@ -514,11 +508,18 @@ kernel(Args a) {
     load_k(now);
     ahead = entries(tile + kWaves);
   }
+  if constexpr (kQInLds) {
+#pragma unroll
+    for (int x = 0; x < kQn; ++x)
+      if (x % kWaves == wave) q_lds[x][lane] = q_reg[x];
+    __syncthreads();
+  }
   for (; tile < tile_end; tile += kWaves) {
     const Rows next = rows_of(ahead);
     ahead = entries(tile + 2 * kWaves);
     load_v(now);
     __builtin_amdgcn_sched_barrier(0);  // they are on their way before the keys are waited for
+    if constexpr (kQInLds) asm volatile("" ::: "memory");  // q is read within the loop
     // ---- S^T = K Q^T ----
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     if constexpr (kLines) {
@@ -550,21 +551,21 @@ kernel(Args a) {
             float f[4];
             floats(C(), p.x[w], f);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t] = mfma16(f[e], qf[x * kCpc + 4 * w + e], s[t]);
+            for (int e = 0; e < 4; ++e) s[t] = mfma16(f[e], __uint_as_float(q_at(4 * x + w)[e]), s[t]);
           }
         } else if constexpr (kF32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t] = mfma16(__uint_as_float(p.x[e]), qf[x * kCpc + e], s[t]);
+          for (int e = 0; e < 4; ++e) s[t] = mfma16(__uint_as_float(p.x[e]), __uint_as_float(q_at(x)[e]), s[t]);
         } else if constexpr (k8) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             uint32_t w0[2], w1[2];
             widen(C(), E16(), p.x[2 * y], w0);
             widen(C(), E16(), p.x[2 * y + 1], w1);
-            s[t] = mfma16(as_x8<E16>(u32x4{w0[0], w0[1], w1[0], w1[1]}), qf[2 * x + y], s[t]);
+            s[t] = mfma16(as_x8<E16>(u32x4{w0[0], w0[1], w1[0], w1[1]}), as_x8<E16>(q_at(2 * x + y)), s[t]);
           }
         } else {
-          s[t] = mfma16(as_x8<E16>(u32x4{p.x[0], p.x[1], p.x[2], p.x[3]}), qf[x], s[t]);
+          s[t] = mfma16(as_x8<E16>(u32x4{p.x[0], p.x[1], p.x[2], p.x[3]}), as_x8<E16>(q_at(x)), s[t]);
         }
       }
     }

@@ -7,18 +7,26 @@
 namespace va {
 namespace paged {
 
-// Workgroups that the cuts should add, where the lengths allow it, to the one that every sequence has for each KV head: 256 CUs hold
-// 768, and up to twice as many even out what sequences of different lengths leave.
-constexpr int kWorkgroups = 1024;
+// Workgroups that the cuts should add, where the lengths allow it, to the one that every sequence has for each KV head.  A few
+// sequences have equal parts, and two workgroups per CU of them are as fast as four (256 CUs hold 768): 131072 keys of 8 heads of 128
+// 85 us with either, but 8.7 or 5.8 for the joining; 4 x 30000 of 2 heads of 256 60 us in all with 1024 and 50 with 512.  Sequences
+// of different lengths leave their last parts, which finer ones even out: 128 of 1024 to 8192 tokens, 8 heads, 232 us with 1024 and
+// 220 with 2048, 33 of 4096, 32 heads of 64, 227 and 213; 4096 gain nothing more.
+constexpr int kWorkgroups = 512, kMoreWorkgroups = 1536, kMorePerPair = 4;
 constexpr int kLeastUnits = 2;
+constexpr int kUncut = 512;    // sequences times KV heads that fill the chip in one piece each
+// Up to this many parts a sequence on average are joined by one wave for each head: 128 sequences, 40 heads, two parts 10.9 -> 4.8 us,
+// 3 sequences of up to eight 3.9 -> 3.4; with 128 parts (one sequence) a workgroup takes 9 us.
 constexpr int kFewParts = 8;
 
 Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
   const int groups = ceil_div(hq / hkv, kHeads);
   const long long least = kLeastUnits * kUnit, most = n_seqs * ((capacity + least - 1) / least);  // parts that there can be
-  const long long each = (long long)hkv * groups, more = std::min<long long>(kWorkgroups, n_seqs * each);
+  const long long each = (long long)hkv * groups, more = std::min<long long>(kMoreWorkgroups, kMorePerPair * n_seqs * each);
   const long long room = (kWorkgroups + more + each - 1) / each;
-  if (capacity <= least) return {n_seqs, kLeastUnits, fast_div(1)};
+  // Short contexts are not cut, which saves the joining: 480 keys, 32/8 heads of 128, one sequence 9.8 -> 8.0 us, 64 of them 27 -> 21;
+  // 900 keys, one sequence 10.1 (uncut 12), 64 of them 45 -> 38: there workgroups are enough without.
+  if (capacity <= (n_seqs * each >= kUncut ? 8 : 4) * kUnit) return {n_seqs, kLeastUnits, fast_div(1)};
   const int extra = (int)std::min(room, most);
   return {n_seqs + extra, kLeastUnits, fast_div(extra)};
 }
@@ -27,7 +35,7 @@ namespace {
 
 // One workgroup per (sequence, query head) adds up the parts' sums, weighted relative to the largest reference exponent: every
 // kJoinRows-th part one group of threads', a column each, and then the groups' sums in order.
-constexpr int kMostParts = 2 * kWorkgroups + 1;  // of one sequence
+constexpr int kMostParts = kWorkgroups + kMoreWorkgroups + 1;  // of one sequence
 
 template <class E, int kCols>  // kCols: threads of a group, d rounded up to 64, 128 or 256
 __global__ void __launch_bounds__(kThreads)

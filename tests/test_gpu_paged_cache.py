@@ -189,7 +189,8 @@ def test_attention(hq, hkv, d, page, dtype, kind):
 @pytest.mark.parametrize("kind", ["plain", "i8", "e4m3"])
 @pytest.mark.parametrize("dtype,lens,page,hq,hkv,d", [
     ("bf16", [5000], 16, 4, 1, 128), ("f16", [4097, 3], 32, 2, 2, 64), ("bf16", [1, 2600, 700, 0], 7, 16, 2, 128),
-    ("f32", [3000], 16, 2, 1, 64), ("bf16", [2049] * 3, 64, 2, 1, 256), ("bf16", [3001, 1], 1, 17, 1, 80)])
+    ("f32", [3000], 16, 2, 1, 64), ("bf16", [2049] * 3, 64, 2, 1, 256), ("bf16", [3001, 1], 1, 17, 1, 80),
+    ("f16", [1500, 20], 24, 3, 1, 33), ("bf16", [1111, 600], 16, 2, 2, 72), ("f32", [900, 2000], 5, 4, 2, 100), ("f16", [1300], 48, 2, 1, 200)])
 def test_long_sequences(dtype, lens, page, hq, hkv, d, kind):
     Setup(dtype, kind, hq, hkv, d, page, lens, seed=len(lens) + page).check()
 
