@@ -95,8 +95,6 @@ struct Row {
 
 // kItems rows of K and of V per kLanes lanes, their loads and look-ups in flight together; workgroup: kItems * kThreads / kLanes
 // consecutive tokens of one head.
-template <class C> constexpr int items() { return is_8bit<C>::value ? 2 : 1; }
-
 template <int kLanes, int kItems> struct Tokens {
   int t[kItems];
   bool there[kItems];
@@ -111,13 +109,12 @@ template <int kLanes, int kItems> struct Tokens {
   }
 };
 
-template <class E, class C, int kVec, int kLanes, bool kWhole>
+template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
              const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  constexpr int kItems = items<C>();
   const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
   const Tokens<kLanes, kItems> tokens(group, N);
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
@@ -150,13 +147,12 @@ write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__r
   }
 }
 
-template <class E, class C, int kVec, int kLanes, bool kWhole>
+template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  constexpr int kItems = items<C>();
   const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
   const Tokens<kLanes, kItems> tokens(group, N);
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
@@ -205,27 +201,36 @@ struct Call {
   hipStream_t stream;
 };
 
-template <class E, class C, int kVec, int kLanes, bool kWhole> hipError_t launch_rows(const Call &a) {
+template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipError_t launch_rows(const Call &a) {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
-  constexpr int kTokens = kThreads / kLanes * items<C>();
+  constexpr int kTokens = kThreads / kLanes * kItems;
   const long long groups = ((long long)a.N + kTokens - 1) / kTokens * a.c.hkv;
   if (groups > 0x7fffffffll) return hipErrorInvalidValue;
   const PageMap map = page_map(a.c);
   const FastDiv heads = fast_div(a.c.hkv);
   if (a.write)
-    write_kernel<E, C, kVec, kLanes, kWhole><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+    write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
         (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
         a.N, heads, a.c.d);
   else
-    read_kernel<E, C, kVec, kLanes, kWhole><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+    read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
         (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
         a.N, heads, a.c.d);
   return hipGetLastError();
 }
 
+// Rows of 8 bits are short enough for two in flight, once there are workgroups to fill the chip: 65536 tokens of 32 heads read back
+// 412 -> 390 us; 20 tokens of 4 heads 3.5, with two 4.1.
+template <class E, class C, int kVec, int kLanes, bool kWhole> hipError_t launch_whole(const Call &a) {
+  constexpr long long kFill = 2048 * 2 * kThreads / kLanes;
+  if constexpr (is_8bit<C>::value && kVec > 1)
+    if ((long long)a.N * a.c.hkv >= kFill) return launch_rows<E, C, kVec, kLanes, kWhole, 2>(a);
+  return launch_rows<E, C, kVec, kLanes, kWhole, 1>(a);
+}
+
 template <class E, class C, int kVec, int kLanes> hipError_t launch(const Call &a) {
-  return kVec > 1 && a.c.d == kVec * kLanes ? launch_rows<E, C, kVec, kLanes, (kVec > 1)>(a) : launch_rows<E, C, kVec, kLanes, false>(a);
+  return kVec > 1 && a.c.d == kVec * kLanes ? launch_whole<E, C, kVec, kLanes, (kVec > 1)>(a) : launch_whole<E, C, kVec, kLanes, false>(a);
 }
 
 // Chunks of 16 bytes of K and V where the rows of both sides consist of whole aligned ones, else single elements.

@@ -286,9 +286,16 @@ template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_
   return p;
 }
 
+// Waves that share a SIMD.  Scattered keys of 8 bits gain from a fourth (33 sequences of 4096, pages of 24, 8 heads of 128: 92 us with
+// three, 78 so); keys that lie together do not (56, 57; 16 bits 95, 110 with four, which spill).
+template <class E, class C> constexpr int waves_per_simd(int dh, Look look) {
+  if (is_f32<E>::value) return dh == 256 ? 1 : 2;
+  return dh == 256 ? 2 : is_8bit<C>::value && look == kPerKey ? 4 : 3;
+}
+
 // E: type of the queries; C: of the cache (E itself or 8 bits); kDh: head_dim rounded up to 64, 128 or 256.
 template <class E, class C, int kDh, Look kLook>
-__global__ void __launch_bounds__(kThreads, is_f32<E>::value ? (kDh == 256 ? 1 : 2) : kDh == 256 ? 2 : 3)
+__global__ void __launch_bounds__(kThreads, (waves_per_simd<E, C>(kDh, kLook)))
 kernel(Args a) {
   constexpr bool kF32 = is_f32<E>::value, k8 = is_8bit<C>::value, kTogether = kLook <= kInPage;  // a product's keys
   typedef typename E::elem elem;
@@ -323,10 +330,11 @@ kernel(Args a) {
   const size_t first_head = (size_t)b * a.hq + g * G + head0;
 
   // q as operand B, head i, the columns of the K chunks: kQn times 16 bytes a lane.  They stay in registers but where
-  // those do not suffice for two waves per SIMD, head_dim 256 of 16 or 32 bits: there every tile reads them from LDS anew (16 sequences
-  // of 500 to 4000 tokens, 16 heads: 114 us with spills, 107 with one wave, 107 so; scattered keys 120, 112, 107).
+  // those do not suffice, head_dim 256 of 16 or 32 bits and the four waves above: there every tile reads them from LDS anew (16
+  // sequences of 500 to 4000 tokens, 16 heads of 256: 114 us with spills, 107 with one wave per SIMD, 107 so; scattered keys 120,
+  // 112, 107).
   constexpr int kEach = 16 / (int)sizeof(elem), kQn = kKn * kCpc / kEach;
-  constexpr bool kQInLds = kDh == 256 && !k8;
+  constexpr bool kQInLds = kDh == 256 ? !k8 : kDh == 128 && waves_per_simd<E, C>(kDh, kLook) == 4;
   __shared__ u32x4 q_lds[kQInLds ? kQn : 1][64];
   u32x4 q_reg[kQn];
   {
