@@ -298,8 +298,9 @@ va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache,
  *   context_lens  : device, [n_seqs] int32, clamped to [0, max_pages * page_size].  Positions whose table entry is no page are
  *                   left out.  A sequence of which nothing is left: O = 0, LSE = -infinity.
  *   softmax_scale : <= 0 means 1 / sqrt(d).
- *   workspace     : >= va_paged_attn_workspace_bytes(...) bytes (may be NULL when that is 0): sums of the parts that long
- *                   sequences are cut into.  Calls that overlap in time need one each.
+ *   workspace     : >= va_paged_attn_workspace_bytes(...) bytes, 16-byte aligned (may be NULL when that is 0): sums of the parts
+ *                   that long sequences are cut into.  Calls that overlap in time need one each.
+ * n_seqs * hkv * ceil(hq / hkv / 16) > 2^23: VA_ERR_UNSUPPORTED.
  * The parts follow from the lengths alone and are joined in order: results are deterministic (no atomics).
  */
 size_t va_paged_attn_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t page_size, int32_t hq, int32_t hkv, int32_t d);

@@ -274,6 +274,8 @@ va_status va_varlen_attn_bwd_noalloc(const void *dO, const void *Q, const void *
 // ---- key-value cache ------------------------------------------------------------------------
 
 namespace {
+constexpr long long kMostTokens = (1ll << 31) - 1024;  // that a sequence's pages hold: a position and a few tiles fit in 31 bits
+
 va_status check_cache(const va_kv_cache *c, va_dtype dt) {
   if (!c) return VA_ERR_NULL;
   if (c->n_pages <= 0 || c->page_size <= 0 || c->hkv <= 0 || c->d <= 0 || c->n_seqs < 0 || c->max_pages < 0) return VA_ERR_SHAPE;
@@ -281,7 +283,7 @@ va_status check_cache(const va_kv_cache *c, va_dtype dt) {
   constexpr long long kMost = 1ll << 31;
   // three factors below 2^31: the first two fit in 64 bits, and are below 2^31 where the third is multiplied
   const long long heads = (long long)c->n_pages * c->hkv;
-  if (heads >= kMost || heads * c->page_size >= kMost || (long long)c->max_pages * c->page_size > kMost - 1024) return VA_ERR_SHAPE;
+  if (heads >= kMost || heads * c->page_size >= kMost || (long long)c->max_pages * c->page_size > kMostTokens) return VA_ERR_SHAPE;
   if ((long long)c->page_size * c->d >= 1ll << 26) return VA_ERR_SHAPE;
   if (dt != VA_F32 && dt != VA_BF16 && dt != VA_F16) return VA_ERR_UNSUPPORTED;
   if (c->format != VA_CACHE_PLAIN && c->format != VA_CACHE_I8 && c->format != VA_CACHE_E4M3) return VA_ERR_UNSUPPORTED;
@@ -318,7 +320,9 @@ va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache,
 
 size_t va_paged_attn_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t page_size, int32_t hq, int32_t hkv, int32_t d) {
   if (n_seqs <= 0 || max_pages <= 0 || page_size <= 0 || hq <= 0 || hkv <= 0 || d <= 0) return 0;
-  return align_up(va::paged_workspace_bytes(n_seqs, (long long)max_pages * page_size, hq, hkv, d));
+  const long long capacity = (long long)max_pages * page_size;
+  if (hq % hkv != 0 || capacity > kMostTokens || n_seqs > 65535 || d > 256) return 0;  // calls that are refused
+  return align_up(va::paged_workspace_bytes(n_seqs, capacity, hq, hkv, d));
 }
 
 va_status va_paged_attn_fwd(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache *cache, int32_t hq,
@@ -327,7 +331,8 @@ va_status va_paged_attn_fwd(const void *Q, void *O, float *LSE, va_dtype dt, con
   const va_status s = check_cache(cache, dt);
   if (s != VA_OK) return s;
   if (hq <= 0 || hq % cache->hkv != 0) return VA_ERR_SHAPE;
-  if (hq > 65535) return VA_ERR_UNSUPPORTED;
+  // a workgroup for each sequence, KV head and 16 of its query heads, and at most as many again
+  if (hq > 65535 || (long long)cache->n_seqs * cache->hkv * ((hq / cache->hkv + 15) / 16) > 1 << 23) return VA_ERR_UNSUPPORTED;
   if (cache->n_seqs == 0) return VA_OK;
   if (!Q || !O || !LSE || !context_lens) return VA_ERR_NULL;
   const size_t need = va_paged_attn_workspace_bytes(cache->n_seqs, cache->max_pages, cache->page_size, hq, cache->hkv, cache->d);

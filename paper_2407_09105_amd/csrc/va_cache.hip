@@ -9,6 +9,8 @@
 // quotient is off.  So 16-bit rows are rounded exactly as real numbers would be, without a division per element.
 //
 // Bound by memory: each element is read once and written once.
+#include <algorithm>
+
 #include "va_kv_cache.h"
 
 namespace va {
@@ -98,11 +100,11 @@ struct Row {
 template <int kLanes, int kItems> struct Tokens {
   int t[kItems];
   bool there[kItems];
-  __device__ __forceinline__ Tokens(long long group, int N) {
+  __device__ __forceinline__ Tokens(int first, long long group, int N) {
     constexpr int kRows = kThreads / kLanes;
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
-      const long long at = (group * kItems + u) * kRows + threadIdx.x / kLanes;
+      const long long at = first + (group * kItems + u) * kRows + threadIdx.x / kLanes;
       there[u] = at < N;
       t[u] = there[u] ? (int)at : N - 1;
     }
@@ -113,10 +115,10 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
-             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(group, N);
+  const Tokens<kLanes, kItems> tokens(first, group, N);
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
   int place[kItems];
 #pragma unroll
@@ -151,10 +153,10 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
-            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int N, FastDiv heads, int d) {
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(group, N);
+  const Tokens<kLanes, kItems> tokens(first, group, N);
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
   int place[kItems];
@@ -205,19 +207,24 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipEr
   typedef typename E::elem elem;
   typedef typename C::elem cached;
   constexpr int kTokens = kThreads / kLanes * kItems;
-  const long long groups = ((long long)a.N + kTokens - 1) / kTokens * a.c.hkv;
-  if (groups > 0x7fffffffll) return hipErrorInvalidValue;
   const PageMap map = page_map(a.c);
   const FastDiv heads = fast_div(a.c.hkv);
-  if (a.write)
-    write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
-        (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-        a.N, heads, a.c.d);
-  else
-    read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
-        (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-        a.N, heads, a.c.d);
-  return hipGetLastError();
+  const long long most = kMostWorkgroups / a.c.hkv * kTokens;  // tokens of a launch
+  for (long long first = 0; first < a.N; first += most) {
+    const long long end = std::min(first + most, (long long)a.N);
+    const unsigned groups = (unsigned)((end - first + kTokens - 1) / kTokens * a.c.hkv);
+    if (a.write)
+      write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+          (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+          (int)first, (int)end, heads, a.c.d);
+    else
+      read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+          (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+          (int)first, (int)end, heads, a.c.d);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Rows of 8 bits are short enough for two in flight, once there are workgroups to fill the chip: 65536 tokens of 32 heads read back

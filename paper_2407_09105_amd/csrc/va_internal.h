@@ -24,6 +24,9 @@ struct Partials {
   size_t bytes;
 };
 
+// Workgroups of 256 threads that one dimension of a launch may have: it counts threads in 32 bits.
+constexpr long long kMostWorkgroups = (1 << 24) - 1;
+
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // va_scan.hip

@@ -24,6 +24,7 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 32;               // keys of a wave's step
 constexpr int kUnit = kTile * kWaves;   // sequences are cut at multiples of this
 constexpr int kHeads = 16;              // query heads of a workgroup
+constexpr int kMostUnits = 1 << 24;     // of the longest sequence, 2^31 tokens
 constexpr float kLazyLog2 = 8.f;
 
 // How the sequences are cut into parts, one workgroup's work per KV head: see find_part.
@@ -75,7 +76,7 @@ __device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, cons
   auto length = [&](int b) { return min(max(lens[min(b, B - 1)], 0), map.capacity); };
   if (split.slots == B) {
     if (slot >= B) return false;
-    part = {slot, slot, 1, 0x7fffffff / kUnit, uniform(length(slot))};
+    part = {slot, slot, 1, kMostUnits, uniform(length(slot))};
     return true;
   }
   const int mine0 = length(lane);
@@ -84,7 +85,8 @@ __device__ __forceinline__ bool find_part(const int32_t *__restrict__ lens, cons
   long long total = __builtin_amdgcn_readlane(sum_upto(units_at(0, mine0)), 63);  // 64 x 2^24 at most
   for (int b0 = 64; b0 < B; b0 += 64) total += __builtin_amdgcn_readlane(sum_upto(units_at(b0, length(b0 + lane))), 63);
   const int drop = total >= 1 << 30 ? 10 : 0;  // to what a 32-bit division takes, rounded up
-  const int c = max(split.least_units, (((int)((total + (1 << drop) - 1) >> drop) + (int)split.extra.d - 1) / split.extra) << drop);
+  const int share = ((int)((total + (1 << drop) - 1) >> drop) + (int)split.extra.d - 1) / split.extra;
+  const int c = max(split.least_units, min(share, kMostUnits >> drop) << drop);
   const float inv = 1.f / (float)c;
   int before = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {

@@ -178,7 +178,7 @@ hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const v
   const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, fast_div(c.hkv), fast_div(groups), hq, G, c.d,
                   scale * 1.4426950408889634f};
   const long long workgroups = ((long long)split.slots * c.hkv + 7) / 8 * 8 * groups;
-  if (workgroups > 0x7fffffffll) return hipErrorInvalidValue;
+  if (workgroups > kMostWorkgroups) return hipErrorInvalidValue;
   (dt == VA_BF16 ? launch_bf16 : dt == VA_F16 ? launch_f16 : launch_f32)(a, c.format, (unsigned)workgroups, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || split.slots == c.n_seqs) return e;

@@ -285,6 +285,20 @@ def test_offsets_past_32_bits():
     check_attention(o, lse, attend64(q, near, small, torch.tensor([n, n])), "bf16", n)
 
 
+def test_more_rows_than_a_launch_has_room_for():
+    """2^28 rows of one element: a launch ends at 2^26 of them."""
+    n, hkv, page = 1 << 22, 64, 64
+    k = torch.arange(n * hkv, device=DEV).remainder(251).to(torch.bfloat16).view(n, hkv, 1)
+    v = -k
+    cache = binding.paged_cache(n // page, page, hkv, 1, torch.bfloat16, DEV)
+    table = torch.arange(n // page, dtype=torch.int32, device=DEV).flip(0)[None]
+    pos, seq = torch.arange(n, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+    binding.paged_cache_write(k, v, cache, table, pos, seq)
+    assert torch.equal(cache.k.flip(0).transpose(1, 2).reshape(n, hkv, 1), k)
+    out = binding.paged_cache_read(cache, table, pos, seq)
+    assert torch.equal(out[0], k) and torch.equal(out[1], v)
+
+
 def test_shared_pages_and_given_outputs():
     """Two sequences with the same prefix pages; outputs and workspace that the caller brings, full of NaN before."""
     s = Setup("bf16", "e4m3", 8, 2, 128, 16, [1000, 100], seed=12)

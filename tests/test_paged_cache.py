@@ -63,6 +63,8 @@ def test_attention_arguments(L):
     assert with_(0, None) == with_(1, None) == with_(2, None) == with_(4, None) == with_(6, None) == 1
     assert with_(3, 7) == 3 and with_(5, 3) == 2 and with_(5, 0) == 2 and with_(5, 65536) == 3
     assert with_(4, C.byref(_cache(n_seqs=0))) == 0
+    assert with_(4, C.byref(_cache(n_pages=1, hkv=129, n_seqs=65535))) == 2              # 4 heads of 129
+    assert f(*ok[:4], C.byref(_cache(n_pages=1, hkv=129, n_seqs=65535)), 129, *ok[6:]) == 3   # too many workgroups
     # one long sequence: shared by many workgroups, which need room
     long = _cache(n_pages=10000, n_seqs=1, max_pages=10000, table_stride=10000)
     need = L.va_paged_attn_workspace_bytes(1, 10000, 16, 4, 2, 64)
@@ -75,6 +77,8 @@ def test_workspace_sizes(L):
     f = L.va_paged_attn_workspace_bytes
     assert f(0, 4, 16, 4, 2, 64) == f(3, 0, 16, 4, 2, 64) == f(3, 4, 16, 4, 2, 0) == f(3, 4, -1, 4, 2, 64) == 0
     assert f(5, 4, 16, 4, 2, 64) == 0                                # short contexts are not cut
+    assert f(5, 1000, 16, 1, 2, 64) == f(5, 1000, 16, 3, 2, 64) == 0  # refused calls need none
+    assert f(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 4, 2, 64) == f(5, 1 << 20, 1 << 20, 4, 2, 64) == 0
     assert f(65535, 1 << 10, 1 << 10, 64, 8, 128) < 8 << 30          # and none takes the card's memory
 
 
