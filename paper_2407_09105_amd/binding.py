@@ -516,7 +516,7 @@ def paged_cache_write(k: torch.Tensor, v: torch.Tensor, cache, page_table: torch
     Tokens without a place (no such sequence, position or page) are left out.  Enqueues one kernel."""
     lib()
     if _native is not None and k.is_cuda:
-        got = _native.cache_write(k, v, cache, page_table, position_ids, seq_ids, torch.cuda.current_device(), _stream())
+        got = _native.cache_write(k, v, cache, page_table, position_ids, seq_ids, _stream())
         if got is not None:
             return _check("va_cache_write", got)
     _check("va_cache_write", lib().va_cache_write(k.data_ptr(), v.data_ptr(),
@@ -532,7 +532,7 @@ def paged_cache_read(cache, page_table: torch.Tensor, position_ids: torch.Tensor
     if out is None:
         dtype = dtype or (torch.bfloat16 if _CACHE_FORMATS.get(pages.dtype) else pages.dtype)
         if _native is not None and pages.is_cuda and dtype in _ROW_TYPES:
-            got = _native.cache_read(cache, page_table, position_ids, seq_ids, _ROW_TYPES[dtype], torch.cuda.current_device(), _stream())
+            got = _native.cache_read(cache, page_table, position_ids, seq_ids, _ROW_TYPES[dtype], _stream())
             if got.__class__ is tuple:
                 return got
             _check("va_cache_read", got or VA_OK)
@@ -553,7 +553,7 @@ def paged_attn_fwd(q: torch.Tensor, cache, page_table: torch.Tensor, context_len
     and -inf.  workspace: float32, of paged_attn_workspace(...)'s size, one for each of several calls that may overlap."""
     lib()
     if _native is not None and out is None and lse is None and workspace is None and q.is_cuda:
-        got = _native.paged(q, cache, page_table, context_lens, float(softmax_scale), torch.cuda.current_device(), _stream())
+        got = _native.paged(q, cache, page_table, context_lens, float(softmax_scale), _stream())
         if got.__class__ is tuple:
             return got
         _check("va_paged_attn_fwd", got or VA_OK)

@@ -13,6 +13,7 @@
 #include <torch/csrc/python_headers.h>
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 
 #include <algorithm>
 
@@ -179,6 +180,8 @@ PyObject *connect_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+int64_t current_device() { return c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index(); }
+
 // A cache (tuple of k, v and their scales or None) and a page table, for rows of type `rows`, all on `device`: the library's view
 // of them, or false where they are not what binding.py asks for.
 bool cache_view(PyObject *cache, PyObject *page_table, at::ScalarType rows, int64_t device, va_kv_cache &c) {
@@ -223,16 +226,17 @@ bool token_ids(PyObject *position_ids, PyObject *seq_ids, int64_t tokens, int64_
   return seq && seq->numel() == tokens && seq->scalar_type() == at::kInt && seq->get_device() == device;
 }
 
-// cache_write(k, v, cache, page_table, position_ids, seq_ids or None, device, stream) -> status | None
+// cache_write(k, v, cache, page_table, position_ids, seq_ids or None, stream) -> status | None
 PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 8) Py_RETURN_NONE;
-  const int64_t device = PyLong_AsLongLong(a[6]);
-  void *stream = PyLong_AsVoidPtr(a[7]);
+  if (n != 7) Py_RETURN_NONE;
+  void *stream = PyLong_AsVoidPtr(a[6]);
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor *k = plain(a[0]), *v = plain(a[1]), *pos, *seq;
+  if (!k || !v) Py_RETURN_NONE;
+  const int64_t device = current_device();
   va_kv_cache c;
-  if (!k || !v || k->dim() != 3 || v->sizes() != k->sizes() || v->scalar_type() != k->scalar_type() || element_type(k->scalar_type()) < 0 ||
+  if ( k->dim() != 3 || v->sizes() != k->sizes() || v->scalar_type() != k->scalar_type() || element_type(k->scalar_type()) < 0 ||
       k->get_device() != device || v->get_device() != device || !cache_view(a[2], a[3], k->scalar_type(), device, c) ||
       k->size(1) != c.hkv || k->size(2) != c.d || k->size(0) > INT32_MAX || !token_ids(a[4], a[5], k->size(0), device, pos, seq))
     Py_RETURN_NONE;
@@ -247,18 +251,20 @@ PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// cache_read(cache, page_table, position_ids, seq_ids or None, type of the rows, device, stream) -> (k, v) | status | None.  The rows
+// cache_read(cache, page_table, position_ids, seq_ids or None, type of the rows, stream) -> (k, v) | status | None.  The rows
 // have the pages' type; out of an 8-bit cache VA_F32, VA_BF16 or VA_F16 as told.
 PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 7) Py_RETURN_NONE;
-  const int64_t type = PyLong_AsLongLong(a[4]), device = PyLong_AsLongLong(a[5]);
-  void *stream = PyLong_AsVoidPtr(a[6]);
+  if (n != 6) Py_RETURN_NONE;
+  const int64_t type = PyLong_AsLongLong(a[4]);
+  void *stream = PyLong_AsVoidPtr(a[5]);
   if (PyErr_Occurred()) return nullptr;
   const at::ScalarType rows = type == VA_F32 ? at::kFloat : type == VA_BF16 ? at::kBFloat16 : at::kHalf;
   const at::Tensor *pos = plain(a[2]), *seq;
+  if (!pos) Py_RETURN_NONE;
+  const int64_t device = current_device();
   va_kv_cache c;
-  if (!pos || pos->numel() > INT32_MAX || !cache_view(a[0], a[1], rows, device, c) || !token_ids(a[2], a[3], pos->numel(), device, pos, seq))
+  if (pos->numel() > INT32_MAX || !cache_view(a[0], a[1], rows, device, c) || !token_ids(a[2], a[3], pos->numel(), device, pos, seq))
     Py_RETURN_NONE;
   at::Tensor k, v;
   va_status status;
@@ -274,17 +280,18 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// paged(q, cache, page_table, context_lens, softmax_scale, device, stream) -> (o, lse) | status | None
+// paged(q, cache, page_table, context_lens, softmax_scale, stream) -> (o, lse) | status | None
 PyObject *paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 7) Py_RETURN_NONE;
+  if (n != 6) Py_RETURN_NONE;
   const float scale = (float)PyFloat_AsDouble(a[4]);
-  const int64_t device = PyLong_AsLongLong(a[5]);
-  void *stream = PyLong_AsVoidPtr(a[6]);
+  void *stream = PyLong_AsVoidPtr(a[5]);
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor *q = plain(a[0]), *lens = plain(a[3]);
+  if (!q || !lens) Py_RETURN_NONE;
+  const int64_t device = current_device();
   va_kv_cache c;
-  if (!q || !lens || q->dim() != 3 || lens->dim() != 1 || element_type(q->scalar_type()) < 0 || lens->scalar_type() != at::kInt ||
+  if (q->dim() != 3 || lens->dim() != 1 || element_type(q->scalar_type()) < 0 || lens->scalar_type() != at::kInt ||
       q->get_device() != device || lens->get_device() != device || !cache_view(a[1], a[2], q->scalar_type(), device, c) ||
       q->size(0) != c.n_seqs || lens->size(0) != c.n_seqs || q->size(2) != c.d || c.hkv <= 0 || q->size(1) % c.hkv != 0 || q->size(1) > INT32_MAX)
     Py_RETURN_NONE;

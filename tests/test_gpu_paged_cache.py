@@ -299,6 +299,50 @@ def test_more_rows_than_a_launch_has_room_for():
     assert torch.equal(out[0], k) and torch.equal(out[1], v)
 
 
+def test_more_sequences_than_cuts():
+    """Thousands of short sequences, some empty, and a long one among them, in a table that would let all be long."""
+    lens = [(31 * b) % 41 for b in range(4099)]
+    lens[4000] = 3100
+    Setup("f16", "e4m3", 3, 1, 8, 16, lens, seed=17, width=200, garbage=False).check()
+
+
+@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+def test_poisoned_rows(kind, page):
+    """A cached row that was not finite (scale NaN) makes its sequence's and KV head's results NaN, and no others'."""
+    s = Setup("bf16", kind, 4, 2, 64, page, [50, 50, 700], seed=8, width=300)
+    clean, clean_lse = s.attend()
+    s.cache[2][s.table[0, 1].item(), 0, 3] = math.nan    # K, heads 0 and 1 of sequence 0
+    s.cache[3][s.table[2, 60].item(), 1, 4] = math.nan   # V, heads 2 and 3 of sequence 2
+    o, lse = s.attend()
+    bad = torch.zeros_like(o, dtype=torch.bool)
+    bad[0, :2] = bad[2, 2:] = True
+    assert torch.isnan(o[bad]).all() and torch.equal(o[~bad], clean[~bad])
+    assert torch.isnan(lse[:2, 0]).all() and torch.equal(lse[2:, 0], clean_lse[2:, 0]) and torch.equal(lse[:, 1:], clean_lse[:, 1:])
+
+
+def test_calls_at_once():
+    """On two streams and from two threads, each with workspaces of its own."""
+    import threading
+    sets = [Setup("bf16", kind, 8, 2, 128, 16, [5000, 7, 900], seed=40 + i, garbage=False) for i, kind in enumerate(("plain", "i8"))]
+    want = [s.attend() for s in sets]
+    got = [[], []]
+    torch.cuda.synchronize()
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got[i].append(sets[i].attend())
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    for i in range(2):
+        assert len(got[i]) == 20 and all(torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1]) for o, lse in got[i])
+
+
 def test_shared_pages_and_given_outputs():
     """Two sequences with the same prefix pages; outputs and workspace that the caller brings, full of NaN before."""
     s = Setup("bf16", "e4m3", 8, 2, 128, 16, [1000, 100], seed=12)
