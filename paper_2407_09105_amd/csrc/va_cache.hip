@@ -23,6 +23,8 @@ __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) 
 }
 
 // kLanes lanes hold a row, lane l its elements l * kVec .. + kVec - 1, or l, l + kLanes, ... (kVec = 1).  kWhole: d is kVec * kLanes.
+// kLanes = 0: d / kVec lanes, whatever that is; no lane idles, but a row cannot be reduced across its lanes (head_dim 96 of 8 heads,
+// 8300 e4m3 tokens read RRR).
 // Stores of whole 128-byte lines pass by the caches (non-temporal; lines that two rows share would be written twice): 65536 tokens
 // of 8 heads of 128 written behind a rotary embedding of K 152 -> 128 us, read back 211 -> 193, and 2 to 3 % slower to 8 % faster
 // together with the next reader of the rows.  Loads do not: the rows to be written have often just left another kernel (16384 of
@@ -31,10 +33,10 @@ template <class E, class C, int kVec, int kLanes, bool kWhole>
 struct Row {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
-  static constexpr int kPer = kVec > 1 ? kVec : 256 / kLanes;   // elements of a lane
+  static constexpr int kPer = kVec > 1 || kLanes == 0 ? kVec : 256 / kLanes;   // elements of a lane
   template <class T> static constexpr bool kPast = kWhole && sizeof(T) * kVec * kLanes % 128 == 0;
   template <class T> using Words = uint32_t __attribute__((ext_vector_type(sizeof(T) * kVec / 4)));
-  static __device__ __forceinline__ int column(int lane, int e) { return kVec > 1 ? lane * kVec + e : lane + e * kLanes; }
+  static __device__ __forceinline__ int column(int lane, int e) { return kVec > 1 || kLanes == 0 ? lane * kVec + e : lane + e * kLanes; }
 
   template <class T> static __device__ __forceinline__ void load(const T *p, int lane, int d, T (&x)[kPer]) {
     if constexpr (kVec > 1) {
@@ -95,17 +97,18 @@ struct Row {
   }
 };
 
-// kItems rows of K and of V per kLanes lanes, their loads and look-ups in flight together; workgroup: kItems * kThreads / kLanes
-// consecutive tokens of one head.
+// kItems rows of K and of V per group of lanes, their loads and look-ups in flight together; workgroup: kItems * (kThreads / lanes of a
+// row) consecutive tokens of one head.
 template <int kLanes, int kItems> struct Tokens {
-  int t[kItems];
+  int lane, t[kItems];
   bool there[kItems];
-  __device__ __forceinline__ Tokens(int first, long long group, int N) {
-    constexpr int kRows = kThreads / kLanes;
+  __device__ __forceinline__ Tokens(int first, long long group, int N, const FastDiv &lanes) {
+    const int tid = threadIdx.x, mine = kLanes ? tid / max(kLanes, 1) : tid / lanes, rows = kThreads / (kLanes ? kLanes : (int)lanes.d);
+    lane = tid - mine * (kLanes ? kLanes : (int)lanes.d);
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
-      const long long at = first + (group * kItems + u) * kRows + threadIdx.x / kLanes;
-      there[u] = at < N;
+      const long long at = first + (group * kItems + u) * rows + mine;
+      there[u] = at < N && mine < rows;
       t[u] = there[u] ? (int)at : N - 1;
     }
   }
@@ -115,10 +118,11 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
-             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, int d) {
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(first, group, N);
+  const int H = heads.d, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
+  const Tokens<kLanes, kItems> tokens(first, group, N, lanes);
+  const int lane = tokens.lane;
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
   int place[kItems];
 #pragma unroll
@@ -153,10 +157,11 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
-            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, int d) {
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  const int H = heads.d, lane = threadIdx.x % kLanes, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(first, group, N);
+  const int H = heads.d, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
+  const Tokens<kLanes, kItems> tokens(first, group, N, lanes);
+  const int lane = tokens.lane;
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
   int place[kItems];
@@ -206,51 +211,63 @@ struct Call {
 template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipError_t launch_rows(const Call &a) {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
-  constexpr int kTokens = kThreads / kLanes * kItems;
+  constexpr bool kWrites = kLanes > 0 || !is_8bit<C>::value, kReads = kLanes == 0 || kWhole;  // see launch_ec
+  const FastDiv heads = fast_div(a.c.hkv), lanes = fast_div(kLanes ? kLanes : a.c.d / kVec);
   const PageMap map = page_map(a.c);
-  const FastDiv heads = fast_div(a.c.hkv);
-  const long long most = kMostWorkgroups / a.c.hkv * kTokens;  // tokens of a launch
+  const int tokens = kThreads / (int)lanes.d * kItems;                                 // of a workgroup
+  const long long most = std::max(kMostWorkgroups / a.c.hkv, 1ll) * tokens;            // of a launch
   for (long long first = 0; first < a.N; first += most) {
     const long long end = std::min(first + most, (long long)a.N);
-    const unsigned groups = (unsigned)((end - first + kTokens - 1) / kTokens * a.c.hkv);
-    if (a.write)
-      write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
-          (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-          (int)first, (int)end, heads, a.c.d);
-    else
-      read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
-          (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-          (int)first, (int)end, heads, a.c.d);
+    const unsigned groups = (unsigned)((end - first + tokens - 1) / tokens * a.c.hkv);
+    if constexpr (kWrites)
+      if (a.write)
+        write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+            (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+            (int)first, (int)end, heads, lanes, a.c.d);
+    if constexpr (kReads)
+      if (!a.write)
+        read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+            (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
+            (int)first, (int)end, heads, lanes, a.c.d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-// Rows of 8 bits are short enough for two in flight, once there are workgroups to fill the chip: 65536 tokens of 32 heads read back
-// 412 -> 390 us; 20 tokens of 4 heads 3.5, with two 4.1.
-template <class E, class C, int kVec, int kLanes, bool kWhole> hipError_t launch_whole(const Call &a) {
-  constexpr long long kFill = 2048 * 2 * kThreads / kLanes;
+// Rows of 8 bits are short enough for two in flight, once there are workgroups for several rounds: 65536 tokens of 32 heads read back
+// 412 -> 390 us; 8300 of 8 heads 11.5, with two 12.7, 20 of 4 heads 3.5 and 4.1.
+template <class E, class C, int kVec, int kLanes, bool kWhole> hipError_t launch(const Call &a) {
+  constexpr long long kFill = 1 << 18;
   if constexpr (is_8bit<C>::value && kVec > 1)
     if ((long long)a.N * a.c.hkv >= kFill) return launch_rows<E, C, kVec, kLanes, kWhole, 2>(a);
   return launch_rows<E, C, kVec, kLanes, kWhole, 1>(a);
 }
 
-template <class E, class C, int kVec, int kLanes> hipError_t launch(const Call &a) {
-  return kVec > 1 && a.c.d == kVec * kLanes ? launch_whole<E, C, kVec, kLanes, (kVec > 1)>(a) : launch_whole<E, C, kVec, kLanes, false>(a);
-}
-
-// Chunks of 16 bytes of K and V where the rows of both sides consist of whole aligned ones, else single elements.
+// Chunks of 16 bytes of K and V where the rows of both sides consist of whole aligned ones, else single elements.  Lanes of a row: 8, 16,
+// 32 or 64 where that is all of it; otherwise as many as it has chunks, unless it is quantised.
 template <class E, class C> hipError_t launch_ec(const Call &a) {
   constexpr int kVec = 16 / sizeof(typename E::elem);
+  constexpr bool k64 = kVec == 4;  // rows of 64 chunks: d <= 256
   const uintptr_t cached_at = (uintptr_t)a.c.k | (uintptr_t)a.c.v, rows_at = (uintptr_t)a.K | (uintptr_t)a.V;
-  if (a.c.d % kVec != 0 || rows_at % 16 != 0 || cached_at % (kVec * sizeof(typename C::elem)) != 0) return launch<E, C, 1, 64>(a);
+  const bool wide = a.c.d % kVec == 0 && rows_at % 16 == 0 && cached_at % (kVec * sizeof(typename C::elem)) == 0;
   const int chunks = a.c.d / kVec;
-  if (chunks <= 8) return launch<E, C, kVec, 8>(a);
-  if (chunks <= 16) return launch<E, C, kVec, 16>(a);
-  if (chunks <= 32) return launch<E, C, kVec, 32>(a);
-  if constexpr (kVec == 4) return launch<E, C, kVec, 64>(a);  // d <= 256
-  else return hipErrorInvalidValue;
+  if (wide) {
+    if (chunks == 8) return launch<E, C, kVec, 8, true>(a);
+    if (chunks == 16) return launch<E, C, kVec, 16, true>(a);
+    if (chunks == 32) return launch<E, C, kVec, 32, true>(a);
+    if constexpr (k64)
+      if (chunks == 64) return launch<E, C, kVec, 64, true>(a);
+  }
+  if constexpr (is_8bit<C>::value) {
+    if (a.write && !wide) return launch<E, C, 1, 64, false>(a);
+    if (a.write && chunks < 8) return launch<E, C, kVec, 8, false>(a);
+    if (a.write && chunks < 16) return launch<E, C, kVec, 16, false>(a);
+    if (a.write && (!k64 || chunks < 32)) return launch<E, C, kVec, 32, false>(a);
+    if constexpr (k64)
+      if (a.write) return launch<E, C, kVec, 64, false>(a);
+  }
+  return wide ? launch<E, C, kVec, 0, false>(a) : launch<E, C, 1, 0, false>(a);
 }
 template <class E> hipError_t launch_e(const Call &a) {
   if (a.c.format == VA_CACHE_I8) return launch_ec<E, I8>(a);
