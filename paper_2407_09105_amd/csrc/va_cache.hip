@@ -24,9 +24,9 @@ __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) 
 
 // kLanes lanes hold a row, lane l its elements l * kVec .. + kVec - 1, or l, l + kLanes, ... (kVec = 1).  kWhole: d is kVec * kLanes.
 // kLanes = 0: d / kVec lanes, whatever that is; no lane idles, but a row cannot be reduced across its lanes (head_dim 96 of 8 heads,
-// 8300 e4m3 tokens read RRR).
-// Stores of whole 128-byte lines pass by the caches (non-temporal; lines that two rows share would be written twice): 65536 tokens
-// of 8 heads of 128 written behind a rotary embedding of K 152 -> 128 us, read back 211 -> 193, and 2 to 3 % slower to 8 % faster
+// 8300 e4m3 tokens read 12.5 -> 10.3 us).
+// kPast: stores of whole 128-byte lines pass by the caches (non-temporal; lines that two workgroups share would be written twice):
+// 65536 tokens of 8 heads of 128 written behind a rotary embedding of K 152 -> 128 us, read back 211 -> 193, and 2 to 3 % slower to 8 % faster
 // together with the next reader of the rows.  Loads do not: the rows to be written have often just left another kernel (16384 of
 // those tokens behind the embedding 35 us, with such loads 38).
 template <class E, class C, int kVec, int kLanes, bool kWhole>
@@ -34,7 +34,6 @@ struct Row {
   typedef typename E::elem elem;
   typedef typename C::elem cached;
   static constexpr int kPer = kVec > 1 || kLanes == 0 ? kVec : 256 / kLanes;   // elements of a lane
-  template <class T> static constexpr bool kPast = kWhole && sizeof(T) * kVec * kLanes % 128 == 0;
   template <class T> using Words = uint32_t __attribute__((ext_vector_type(sizeof(T) * kVec / 4)));
   static __device__ __forceinline__ int column(int lane, int e) { return kVec > 1 || kLanes == 0 ? lane * kVec + e : lane + e * kLanes; }
 
@@ -55,14 +54,14 @@ struct Row {
       for (int e = 0; e < kPer; ++e) x[e] = column(lane, e) < d ? p[column(lane, e)] : (T)0;
     }
   }
-  template <class T> static __device__ __forceinline__ void store(T *p, int lane, int d, const T (&x)[kPer]) {
+  template <bool kPast, class T> static __device__ __forceinline__ void store(T *p, int lane, int d, const T (&x)[kPer]) {
     if constexpr (kVec > 1) {
       struct Chunk { T x[kVec]; } c;
       if (kWhole || lane * kVec < d) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) c.x[e] = x[e];
         Words<T> *const at = (Words<T> *)(p + lane * kVec);
-        if (kPast<T>) __builtin_nontemporal_store(__builtin_bit_cast(Words<T>, c), at);
+        if constexpr (kPast) __builtin_nontemporal_store(__builtin_bit_cast(Words<T>, c), at);
         else *at = __builtin_bit_cast(Words<T>, c);
       }
     } else {
@@ -97,19 +96,25 @@ struct Row {
   }
 };
 
-// kItems rows of K and of V per group of lanes, their loads and look-ups in flight together; workgroup: kItems * (kThreads / lanes of a
-// row) consecutive tokens of one head.
-template <int kLanes, int kItems> struct Tokens {
-  int lane, t[kItems];
+// What a thread works on: kItems rows of K and of V, their loads and look-ups in flight together, and its place in them.  Workgroups
+// take consecutive tokens of one head (neighbours in a page, and in K and V where a row is whole lines), or, kInOrder, consecutive
+// rows of K and V, so that lines that rows share are stored by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 ->
+// 190 us, e4m3 rows of 96 85 -> 81.
+template <int kLanes, int kItems, bool kInOrder> struct Work {
+  int lane, t[kItems], g[kItems];  // token, head
   bool there[kItems];
-  __device__ __forceinline__ Tokens(int first, long long group, int N, const FastDiv &lanes) {
-    const int tid = threadIdx.x, mine = kLanes ? tid / max(kLanes, 1) : tid / lanes, rows = kThreads / (kLanes ? kLanes : (int)lanes.d);
-    lane = tid - mine * (kLanes ? kLanes : (int)lanes.d);
+  __device__ __forceinline__ Work(int first, int N, const FastDiv &heads, const FastDiv &lanes) {
+    const int H = heads.d, tid = threadIdx.x, per_row = kLanes ? kLanes : (int)lanes.d, rows = kThreads / per_row;
+    const int mine = kLanes ? tid / (kLanes ? kLanes : 1) : tid / lanes;  // row of this thread
+    const int group = (int)blockIdx.x / heads, head = (blockIdx.x - group * H + group) % heads;  // heads in turn across XCDs
+    lane = tid - mine * per_row;
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
-      const long long at = first + (group * kItems + u) * rows + mine;
-      there[u] = at < N && mine < rows;
-      t[u] = there[u] ? (int)at : N - 1;
+      const long long at = ((long long)(kInOrder ? (int)blockIdx.x : group) * kItems + u) * rows + mine;  // row or token
+      there[u] = mine < rows && at < (kInOrder ? (long long)(N - first) * H : N - first);
+      const int x = there[u] ? (int)at : 0;
+      t[u] = first + (kInOrder ? x / heads : x);
+      g[u] = kInOrder ? x % heads : head;
     }
   }
 };
@@ -120,35 +125,36 @@ write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__r
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
              const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  const int H = heads.d, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(first, group, N, lanes);
-  const int lane = tokens.lane;
+  constexpr bool kPast = kWhole && sizeof(typename C::elem) * kVec * kLanes % 128 == 0;
+  const int H = heads.d;
+  const Work<kLanes, kItems, false> work(first, N, heads, lanes);
+  const int lane = work.lane;
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
   int place[kItems];
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
-    const size_t from = ((size_t)tokens.t[u] * H + g) * d;
+    const size_t from = ((size_t)work.t[u] * H + work.g[u]) * d;
     R::load(K + from, lane, d, k[u]);
     R::load(V + from, lane, d, v[u]);
-    place[u] = place_of(map, seq_ids ? seq_ids[tokens.t[u]] : tokens.t[u], id_at(pos, it, tokens.t[u]));
+    place[u] = place_of(map, seq_ids ? seq_ids[work.t[u]] : work.t[u], id_at(pos, it, work.t[u]));
   }
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
-    if (!tokens.there[u] || place[u] < 0) continue;
-    const size_t row = (size_t)place[u] + (size_t)g * map.page.d;
+    if (!work.there[u] || place[u] < 0) continue;
+    const size_t row = (size_t)place[u] + (size_t)work.g[u] * map.page.d;
     if constexpr (is_8bit<C>::value) {
       typename C::elem q[R::kPer];
       const float sk = R::quantise(k[u], q);
-      R::store(Kc + row * d, lane, d, q);
+      R::template store<kPast>(Kc + row * d, lane, d, q);
       const float sv = R::quantise(v[u], q);
-      R::store(Vc + row * d, lane, d, q);
+      R::template store<kPast>(Vc + row * d, lane, d, q);
       if (lane == 0) {
         ks[row] = sk;
         vs[row] = sv;
       }
     } else {
-      R::store(Kc + row * d, lane, d, k[u]);
-      R::store(Vc + row * d, lane, d, v[u]);
+      R::template store<kPast>(Kc + row * d, lane, d, k[u]);
+      R::template store<kPast>(Vc + row * d, lane, d, v[u]);
     }
   }
 }
@@ -159,25 +165,26 @@ read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, 
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
-  const int H = heads.d, group = (int)blockIdx.x / heads, g = (blockIdx.x - group * H + group) % heads;
-  const Tokens<kLanes, kItems> tokens(first, group, N, lanes);
-  const int lane = tokens.lane;
+  constexpr bool kInOrder = kLanes == 0, kPast = kInOrder ? kVec > 1 : sizeof(typename E::elem) * kVec * kLanes % 128 == 0;
+  const int H = heads.d;
+  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes);
+  const int lane = work.lane;
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
   int place[kItems];
 #pragma unroll
   for (int u = 0; u < kItems; ++u)
-    place[u] = place_of(map, seq_ids ? seq_ids[tokens.t[u]] : tokens.t[u], id_at(pos, it, tokens.t[u]));
+    place[u] = place_of(map, seq_ids ? seq_ids[work.t[u]] : work.t[u], id_at(pos, it, work.t[u]));
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
-    const size_t row = (size_t)max(place[u], 0) + (size_t)g * map.page.d;  // of page 0 where there is none
+    const size_t row = (size_t)max(place[u], 0) + (size_t)work.g[u] * map.page.d;  // of page 0 where there is none
     R::load(Kc + row * d, lane, d, k[u]);
     R::load(Vc + row * d, lane, d, v[u]);
     if constexpr (is_8bit<C>::value) sk[u] = ks[row], sv[u] = vs[row];
   }
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
-    if (!tokens.there[u]) continue;
+    if (!work.there[u]) continue;
     typename E::elem x[R::kPer], y[R::kPer];
 #pragma unroll
     for (int e = 0; e < R::kPer; ++e) {
@@ -191,9 +198,9 @@ read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, 
         }
       }
     }
-    const size_t to = ((size_t)tokens.t[u] * H + g) * d;
-    R::store(K + to, lane, d, x);
-    R::store(V + to, lane, d, y);
+    const size_t to = ((size_t)work.t[u] * H + work.g[u]) * d;
+    R::template store<kPast>(K + to, lane, d, x);
+    R::template store<kPast>(V + to, lane, d, y);
   }
 }
 
@@ -214,11 +221,13 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipEr
   constexpr bool kWrites = kLanes > 0 || !is_8bit<C>::value, kReads = kLanes == 0 || kWhole;  // see launch_ec
   const FastDiv heads = fast_div(a.c.hkv), lanes = fast_div(kLanes ? kLanes : a.c.d / kVec);
   const PageMap map = page_map(a.c);
-  const int tokens = kThreads / (int)lanes.d * kItems;                                 // of a workgroup
-  const long long most = std::max(kMostWorkgroups / a.c.hkv, 1ll) * tokens;            // of a launch
+  const int rows = kThreads / (int)lanes.d * kItems;                                   // of a workgroup
+  // tokens of a launch: its workgroups, and its rows in 31 bits
+  const long long most = std::min(kMostWorkgroups / a.c.hkv * rows, 0x7fffffffll / a.c.hkv);
   for (long long first = 0; first < a.N; first += most) {
     const long long end = std::min(first + most, (long long)a.N);
-    const unsigned groups = (unsigned)((end - first + tokens - 1) / tokens * a.c.hkv);
+    const bool in_order = !a.write && kLanes == 0;
+    const unsigned groups = (unsigned)(in_order ? ((end - first) * a.c.hkv + rows - 1) / rows : (end - first + rows - 1) / rows * a.c.hkv);
     if constexpr (kWrites)
       if (a.write)
         write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
