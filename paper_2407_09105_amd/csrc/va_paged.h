@@ -1,19 +1,24 @@
 // Attention of one new token of every sequence over the paged key-value cache: the kernel (instantiated in va_paged_*.hip, one
 // file per type of the queries) and what it shares with the joining of parts (va_paged.hip).
 //
-// A wave takes 32 keys at a time for the (up to 16) query heads of a KV head, straight from memory into registers: no LDS, no
-// barrier, until the waves' results are joined at the end.  With v_mfma_f32_16x16x32 (lane l: i = l % 16, h = l / 16; operand
-// A row i, B column i, both at k = 8 h + 0..7; result: column i, rows 4 h + 0..3):
-//   - S^T = K Q^T, two products of 16 keys: lane (i, h) loads 16-byte chunks h, h + 4, ... of key i's row - which columns share a
-//     k-step does not matter as long as q's fragments hold the same ones - and ends up with scores of head i, keys 4 h + 0..3.
+// A wave takes 32 keys at a time for the (up to 16) query heads of a KV head, straight from memory into registers: no barrier, and no
+// LDS but for the queries where registers do not hold them, until the waves' results are joined at the end.  With
+// v_mfma_f32_16x16x32 (lane l: i = l % 16, h = l / 16; operand A row i, B column i, both at k = 8 h + 0..7; result: column i, rows
+// 4 h + 0..3):
+//   - S^T = K Q^T, two products of 16 keys: lane (i, h) holds 16-byte chunks h, h + 4, ... of key i's row (loaded as whole 128-byte
+//     lines, then swapped between lanes 8 apart) - which columns share a k-step does not matter as long as q's fragments hold the
+//     same ones - and ends up with scores of head i, keys 4 h + 0..3.
 //   - O^T += V^T P^T: those 2 x 4 keys are k = 8 h + 0..7, so P^T needs no exchange between lanes.  Lane (i, h) loads columns
 //     8 i + 0..7 of its 8 keys (16 lanes together a whole row of 128 columns); the fragment of the m-th product, whose rows are the
 //     columns 8 i + m, is the m-th element of each of them: four byte permutations, half an instruction per element.
+// fp32 queries do both products with v_mfma_f32_16x16x4_f32, an element of a lane's chunk per step.
 // Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  P enters the
 // matrix unit in two 16-bit parts (the second holds what the first cuts off, 2^-15 of P remain): the matrix unit is idle nine
 // tenths of the time, and the result is as exact as fp32 probabilities make it.
 //
-// Bound by memory: keys and values are read once, 2 d bytes each against 4 d flops per query head.
+// Bound by memory: keys and values are read once, 2 d elements each key against 4 d flops per query head.  Measured, with the
+// joining: 131072 keys of 8 heads of 128 in bf16 87 us (6.1 TB/s; the kernel alone 6.6, the card reads 7.0), 128 sequences of
+// 1024 to 8192 in e4m3 221 us (5.9), 16 of up to 4096 with 16 heads of 256 113 us (5.7).
 #pragma once
 #include "va_kv_cache.h"
 
