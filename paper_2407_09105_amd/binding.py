@@ -446,7 +446,7 @@ class PagedCache(NamedTuple):
 _CACHE_FORMATS = {torch.float32: CACHE_PLAIN, torch.bfloat16: CACHE_PLAIN, torch.float16: CACHE_PLAIN, torch.int8: CACHE_I8,
                   torch.float8_e4m3fn: CACHE_E4M3}
 
-
+_INT32_MAX = 2 ** 31 - 1
 _ROW_TYPES = {torch.float32: VA_F32, torch.bfloat16: VA_BF16, torch.float16: VA_F16}
 
 
@@ -488,6 +488,8 @@ def _kv_cache(cache, page_table: torch.Tensor, dtype: torch.dtype, *others) -> V
     for t in tensors:
         if t.device.index != here:
             raise ValueError(f"a tensor lives on {t.device}, the current device is cuda:{here}")
+    if max(*k.shape, seqs, width) > _INT32_MAX:
+        raise ValueError("a cache's or a page table's sizes must fit 32 bits")
     scales = (None, None) if fmt == CACHE_PLAIN else (k_scale.data_ptr(), v_scale.data_ptr())
     n_pages, hkv, page_size, d = k.shape
     return VaKvCache(k.data_ptr(), v.data_ptr(), *scales, n_pages, page_size, hkv, d, fmt, seqs, width, stride, page_table.data_ptr())
@@ -500,6 +502,8 @@ def _cache_rows(k, v, cache, page_table, position_ids, seq_ids):
     if k.dim() != 3 or v.shape != k.shape or v.dtype != k.dtype or k.shape[1:] != (c.hkv, c.d):
         raise ValueError(f"expected K, V [N, {c.hkv}, {c.d}] of one dtype")
     N = k.shape[0]
+    if N > _INT32_MAX:
+        raise ValueError("more tokens than a call takes")
     if position_ids.numel() != N or position_ids.dtype not in (torch.int32, torch.int64):
         raise ValueError(f"expected {N} position ids, int32 or int64")
     if seq_ids is not None and (seq_ids.numel() != N or seq_ids.dtype != torch.int32):

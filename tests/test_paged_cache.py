@@ -162,3 +162,28 @@ def test_paged_cache_on_the_cpu_is_refused(L):
         binding.paged_cache(4, 16, 2, 64, torch.float64, "cpu")
     with pytest.raises(ValueError, match="GPU"):
         binding.paged_attn_fwd(torch.zeros(1, 2, 64), cache, torch.zeros(1, 1, dtype=torch.int32), torch.ones(1, dtype=torch.int32))
+
+
+def test_sizes_past_32_bits_are_refused(L, monkeypatch):
+    """(ctypes would pass on their lower halves)"""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with FakeTensorMode():
+        of = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, device="cuda:0", dtype=dtype)  # noqa: E731
+        for many in (2 ** 31, 2 ** 32 + 1):
+            table, pos = of(3, 4, dtype=torch.int32), of(8, dtype=torch.int64)
+            for pages in ((many, 1, 1, 1), (1, many, 1, 1), (1, 1, many, 1), (1, 1, 1, many)):
+                cache = (of(*pages), of(*pages), None, None)
+                with pytest.raises(ValueError, match="32 bits"):
+                    binding.paged_attn_fwd(of(3, pages[1], pages[3]), cache, table, of(3, dtype=torch.int32))
+                with pytest.raises(ValueError, match="32 bits"):
+                    binding.paged_cache_read(cache, table, pos)
+            cache = (of(10, 1, 16, 1), of(10, 1, 16, 1), None, None)
+            for table in (of(3, many, dtype=torch.int32), of(many, 4, dtype=torch.int32)):
+                with pytest.raises(ValueError, match="32 bits"):
+                    binding.paged_cache_read(cache, table, pos)
+            with pytest.raises(ValueError, match="more tokens"):
+                binding.paged_cache_write(of(many, 1, 1), of(many, 1, 1), cache, of(3, 4, dtype=torch.int32), of(many, dtype=torch.int64))
+            with pytest.raises(ValueError, match="more tokens"):
+                binding.paged_cache_read(cache, of(3, 4, dtype=torch.int32), of(many, dtype=torch.int64))
