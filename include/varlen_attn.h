@@ -300,6 +300,7 @@ va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache,
  *   softmax_scale : <= 0 means 1 / sqrt(d).
  *   workspace     : >= va_paged_attn_workspace_bytes(...) bytes, 16-byte aligned (may be NULL when that is 0): sums of the parts
  *                   that long sequences are cut into.  Calls that overlap in time need one each.
+ * P V is summed in fp32 before it is divided by the sum of P: elements of V whose n-fold exceeds 10^36 may overflow to infinity.
  * n_seqs * hkv * ceil(hq / hkv / 16) > 2^23: VA_ERR_UNSUPPORTED.
  * The parts follow from the lengths alone and are joined in order: results are deterministic (no atomics).
  */
