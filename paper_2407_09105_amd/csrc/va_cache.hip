@@ -17,6 +17,7 @@ namespace va {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kSpread = 64;  // groups of tokens that are spread well enough over the 8 XCDs, whole groups at a time
 
 __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) {
   return it == VA_I64 ? (long long)((const int64_t *)ids)[t] : (long long)((const int32_t *)ids)[t];
@@ -99,14 +100,19 @@ struct Row {
 // What a thread works on: kItems rows of K and of V, their loads and look-ups in flight together, and its place in them.  Workgroups
 // take consecutive tokens of one head (neighbours in a page, and in K and V where a row is whole lines), or, kInOrder, consecutive
 // rows of K and V, so that lines that rows share are stored by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 ->
-// 190 us, e4m3 rows of 96 85 -> 81.
+// 190 us, e4m3 rows of 96 85 -> 81.  together: all heads of a group of tokens on one XCD, whose L2 then serves both heads that share a
+// line (60000 tokens of 32 heads of 80 written: bf16 into pages of 16 252 -> 240 us, pages of one 363 -> 248, int8 there 336 -> 291).
 template <int kLanes, int kItems, bool kInOrder> struct Work {
   int lane, t[kItems], g[kItems];  // token, head
   bool there[kItems];
-  __device__ __forceinline__ Work(int first, int N, const FastDiv &heads, const FastDiv &lanes) {
+  __device__ __forceinline__ Work(int first, int N, const FastDiv &heads, const FastDiv &lanes, bool together) {
     const int H = heads.d, tid = threadIdx.x, per_row = kLanes ? kLanes : (int)lanes.d, rows = kThreads / per_row;
     const int mine = kLanes ? tid / (kLanes ? kLanes : 1) : tid / lanes;  // row of this thread
-    const int group = (int)blockIdx.x / heads, head = (blockIdx.x - group * H + group) % heads;  // heads in turn across XCDs
+    int group = (int)blockIdx.x / heads, head = (blockIdx.x - group * H + group) % heads;  // heads in turn across XCDs
+    if (together) {
+      const int turn = blockIdx.x >> 3, eighth = turn / heads;
+      group = eighth * 8 + (blockIdx.x & 7), head = turn - eighth * H;
+    }
     lane = tid - mine * per_row;
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
@@ -123,11 +129,12 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
-             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d,
+             bool together) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   constexpr bool kPast = kWhole && sizeof(typename C::elem) * kVec * kLanes % 128 == 0;
   const int H = heads.d;
-  const Work<kLanes, kItems, false> work(first, N, heads, lanes);
+  const Work<kLanes, kItems, false> work(first, N, heads, lanes, together);
   const int lane = work.lane;
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
   int place[kItems];
@@ -167,7 +174,7 @@ read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, 
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   constexpr bool kInOrder = kLanes == 0, kPast = kInOrder ? kVec > 1 : sizeof(typename E::elem) * kVec * kLanes % 128 == 0;
   const int H = heads.d;
-  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes);
+  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes, false);
   const int lane = work.lane;
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
@@ -222,20 +229,23 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipEr
   const FastDiv heads = fast_div(a.c.hkv), lanes = fast_div(kLanes ? kLanes : a.c.d / kVec);
   const PageMap map = page_map(a.c);
   const int rows = kThreads / (int)lanes.d * kItems;                                   // of a workgroup
-  // tokens of a launch: its workgroups, and its rows in 31 bits
-  const long long most = std::min(kMostWorkgroups / a.c.hkv * rows, 0x7fffffffll / a.c.hkv);
+  // tokens of a launch: its workgroups (rounded up, see below), and its rows in 31 bits
+  const long long most = std::min((kMostWorkgroups / a.c.hkv - 7) * rows, 0x7fffffffll / a.c.hkv);
   for (long long first = 0; first < a.N; first += most) {
     const long long end = std::min(first + most, (long long)a.N);
     const bool in_order = !a.write && kLanes == 0;
-    const unsigned groups = (unsigned)(in_order ? ((end - first) * a.c.hkv + rows - 1) / rows : (end - first + rows - 1) / rows * a.c.hkv);
+    long long groups = (end - first + rows - 1) / rows;
+    const bool together = a.write && !kWhole && groups >= kSpread;
+    if (together) groups = (groups + 7) / 8 * 8;
+    groups = in_order ? ((end - first) * a.c.hkv + rows - 1) / rows : groups * a.c.hkv;
     if constexpr (kWrites)
       if (a.write)
-        write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+        write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
             (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-            (int)first, (int)end, heads, lanes, a.c.d);
+            (int)first, (int)end, heads, lanes, a.c.d, together);
     if constexpr (kReads)
       if (!a.write)
-        read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<groups, kThreads, 0, a.stream>>>(
+        read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
             (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
             (int)first, (int)end, heads, lanes, a.c.d);
     const hipError_t e = hipGetLastError();

@@ -90,6 +90,40 @@ def test_write_and_read(d, hkv, page, dtype, kind):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("kind", ["plain", "i8", "e4m3"])
+@pytest.mark.parametrize("d,hkv,dtype,lens", [(80, 3, "bf16", [1500, 1, 1200]), (96, 2, "f16", [2000, 333]), (33, 2, "f32", [501, 600]),
+                                              (72, 5, "f16", [2100]), (24, 1, "bf16", [9000]), (100, 1, "f32", [2500]), (8, 64, "bf16", [4200])])
+def test_many_rows_of_odd_sizes(d, hkv, dtype, lens, kind):
+    """Streams of many groups of tokens, the last of them ragged, rows that share memory lines with their neighbours'."""
+    page = 13
+    table, pos, seq, n_pages = _stream(lens, page, seed=d, pad=3)
+    k, v = _rows(len(pos), hkv, d, dtype, seed=d + 7)
+    cache = binding.paged_cache(n_pages, page, hkv, d, cache_dtype(dtype, kind), DEV)
+    order = torch.randperm(len(pos), generator=torch.Generator().manual_seed(9))   # tokens of one page far apart
+    binding.paged_cache_write(k[order.to(DEV)], v[order.to(DEV)], cache, table.to(DEV), pos[order].to(DEV), seq[order].to(DEV))
+    n = sum(lens)
+    pages, rows = table[seq[:n].long(), pos[:n] // page].long(), pos[:n] % page
+    for i, x in enumerate((k, v)):
+        want, scale = (x[:n].cpu().double(), None) if kind == "plain" else quantise64(x[:n].cpu().double(), kind)
+        got = cache[i].cpu().float().double()[pages, :, rows]
+        if dtype == "f32" and kind != "plain":   # as in test_write_and_read
+            off = (got - want).abs()
+            assert (off <= torch.maximum(want.abs() / 8, torch.tensor(1.0))).all() and (off > 0).double().mean() < 1e-3
+        else:
+            assert torch.equal(got, want)
+        if scale is not None:
+            assert ((cache[2 + i].cpu().double()[pages, :, rows] - scale).abs() <= 2.0 ** -23 * scale).all()
+        used = torch.zeros(n_pages, page, dtype=torch.bool)
+        used[pages, rows] = True
+        assert (cache[i].cpu().float().transpose(1, 2)[~used] == 0).all()
+    out = binding.paged_cache_read(cache, table.to(DEV), pos.to(DEV), seq.to(DEV), dtype=DTYPES[dtype])
+    for i in range(2):
+        want = values64(cache[i], cache[2 + i])[pages, :, rows]
+        got = out[i].cpu().double()
+        assert (got[n:] == 0).all()
+        assert ((got[:n] - want).abs() <= (torch.finfo(DTYPES[dtype]).eps / 2 + 2.0 ** -23) * want.abs() + torch.finfo(DTYPES[dtype]).tiny).all()
+
+
 @pytest.mark.parametrize("kind", ["i8", "e4m3"])
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_rows_that_are_hard_to_quantise(dtype, kind):
