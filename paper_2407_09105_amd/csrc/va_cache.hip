@@ -97,11 +97,12 @@ struct Row {
   }
 };
 
-// What a thread works on: kItems rows of K and of V, their loads and look-ups in flight together, and its place in them.  Workgroups
-// take consecutive tokens of one head (neighbours in a page, and in K and V where a row is whole lines), or, kInOrder, consecutive
-// rows of K and V, so that lines that rows share are stored by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 ->
-// 190 us, e4m3 rows of 96 85 -> 81.  together: all heads of a group of tokens on one XCD, whose L2 then serves both heads that share a
-// line (60000 tokens of 32 heads of 80 written: bf16 into pages of 16 252 -> 240 us, pages of one 363 -> 248, int8 there 336 -> 291).
+// What a thread works on: kItems rows of K and of V, their loads and look-ups in flight together, and its place in them.  A group of
+// tokens has as many workgroups as there are heads, which take one head each (neighbours in a page, and in K and V where a row is
+// whole lines), or, kInOrder, an equal part of the group's rows in the order of K and V, so that lines that rows share are stored
+// by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 -> 190 us, e4m3 rows of 96 85 -> 81.  together: the workgroups of a
+// group on one XCD, whose L2 then serves both that share a line (60000 tokens of 32 heads of 80 written: bf16 into pages of 16 252 ->
+// 240 us, pages of one 363 -> 248, int8 there 336 -> 291; 8300 e4m3 rows of 8 heads of 96 read 10.4 -> 9.4, fp32 rows of 33 110 -> 103).
 template <int kLanes, int kItems, bool kInOrder> struct Work {
   int lane, t[kItems], g[kItems];  // token, head
   bool there[kItems];
@@ -114,13 +115,17 @@ template <int kLanes, int kItems, bool kInOrder> struct Work {
       group = eighth * 8 + (blockIdx.x & 7), head = turn - eighth * H;
     }
     lane = tid - mine * per_row;
+    const long long tokens = N - first, begin = (long long)group * (rows * kItems);
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
-      const long long at = ((long long)(kInOrder ? (int)blockIdx.x : group) * kItems + u) * rows + mine;  // row or token
-      there[u] = mine < rows && at < (kInOrder ? (long long)(N - first) * H : N - first);
-      const int x = there[u] ? (int)at : 0;
-      t[u] = first + (kInOrder ? x / heads : x);
-      g[u] = kInOrder ? x % heads : head;
+      long long at = begin + u * rows + mine;
+      g[u] = head;
+      if constexpr (kInOrder) {  // the head-th part of the rows of the group's tokens
+        const int row = (head * kItems + u) * rows + mine, token = row / heads;
+        at = begin + token, g[u] = row - token * H;
+      }
+      there[u] = mine < rows && at < tokens;
+      t[u] = first + (there[u] ? (int)at : 0);
     }
   }
 };
@@ -170,11 +175,12 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
-            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d,
+            bool together) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   constexpr bool kInOrder = kLanes == 0, kPast = kInOrder ? kVec > 1 : sizeof(typename E::elem) * kVec * kLanes % 128 == 0;
   const int H = heads.d;
-  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes, false);
+  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes, together);
   const int lane = work.lane;
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
@@ -233,21 +239,20 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipEr
   const long long most = std::min((kMostWorkgroups / a.c.hkv - 7) * rows, 0x7fffffffll / a.c.hkv);
   for (long long first = 0; first < a.N; first += most) {
     const long long end = std::min(first + most, (long long)a.N);
-    const bool in_order = !a.write && kLanes == 0;
     long long groups = (end - first + rows - 1) / rows;
-    const bool together = a.write && !kWhole && groups >= kSpread;
+    const bool together = !kWhole && groups >= kSpread;
     if (together) groups = (groups + 7) / 8 * 8;
-    groups = in_order ? ((end - first) * a.c.hkv + rows - 1) / rows : groups * a.c.hkv;
+    const unsigned workgroups = (unsigned)(groups * a.c.hkv);
     if constexpr (kWrites)
       if (a.write)
-        write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+        write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<workgroups, kThreads, 0, a.stream>>>(
             (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
             (int)first, (int)end, heads, lanes, a.c.d, together);
     if constexpr (kReads)
       if (!a.write)
-        read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<(unsigned)groups, kThreads, 0, a.stream>>>(
+        read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<workgroups, kThreads, 0, a.stream>>>(
             (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-            (int)first, (int)end, heads, lanes, a.c.d);
+            (int)first, (int)end, heads, lanes, a.c.d, together);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
