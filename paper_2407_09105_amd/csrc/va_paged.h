@@ -192,8 +192,11 @@ template <> struct shift_log2<F16> { static constexpr float value = 6.f; };
 //   kWholeRows: page_size is a multiple of 16, so that the 16 keys of a product lie next to each other, and head_dim is kDh itself
 //   kInPage:    the pages likewise, any head_dim that 16-byte chunks fit
 //   kPerKey:    each key is found on its own
-//   kElements:  likewise, and rows are read in dwords or single elements (head dims or addresses that 16-byte chunks do not fit)
-enum Look { kWholeRows, kInPage, kPerKey, kElements };
+//   kDwords:    likewise, and rows are at least four whole dwords, which 16-byte chunks do not fit: the chunk that a row ends in is
+//               loaded from its end and moved (82 sequences of 4259, 4 heads of 33 fp32 elements: 223 us in single dwords, 95 so;
+//               30 of 4000, 8 heads of 100 bf16 elements 132, 81)
+//   kElements:  likewise, and rows are read element by element
+enum Look { kWholeRows, kInPage, kPerKey, kDwords, kElements };
 
 struct Args {
   const void *Q;
@@ -265,15 +268,25 @@ template <int kBytes> __device__ __forceinline__ Piece<kBytes> memory_piece(cons
   for (int i = 0; i < kBytes / 4; ++i) q.x[i] = r.x[i];
   return q;
 }
-// elements `column` .. of a row of d elements, zeros behind it; dwords: rows begin and end at whole dwords
-template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_piece(const T *row, int column, int d, bool dwords) {
+// A row's bytes from `at` on, which may end inside the piece: the row's last kBytes, its words moved down once they are here.
+template <int kBytes> __device__ __forceinline__ Piece<kBytes> last_piece(const char *row, int at, int row_bytes) {
+  return memory_piece<kBytes>(row + min(at, row_bytes - kBytes));
+}
+template <int kBytes> __device__ __forceinline__ void move_down(Piece<kBytes> &p, int at, int row_bytes) {
+  const int by = max(at - (row_bytes - kBytes), 0) / 4;  // what moves in at the end is not there: any value
+  constexpr int kWords = kBytes / 4;
+#pragma unroll
+  for (int step = 1; step < kWords; step *= 2)
+#pragma unroll
+    for (int w = 0; w + step < kWords; ++w) {
+      const uint32_t here = p.x[w], next = p.x[w + step];
+      p.x[w] = (by & step) != 0 ? next : here;
+    }
+}
+// elements `column` .. of a row of d elements, zeros behind it
+template <class T, int kBytes> __device__ __forceinline__ Piece<kBytes> element_piece(const T *row, int column, int d) {
   constexpr int kEach = 4 / sizeof(T);
   Piece<kBytes> p;
-  if (dwords) {
-#pragma unroll
-    for (int i = 0; i < kBytes / 4; ++i) p.x[i] = column + i * kEach < d ? *(const uint32_t *)(row + column + i * kEach) : 0u;
-    return p;
-  }
 #pragma unroll
   for (int i = 0; i < kBytes / 4; ++i) {
     uint32_t w = 0;
@@ -350,8 +363,8 @@ kernel(Args a) {
     for (int x = 0; x < kQn; ++x) {
       const int column = (4 * (x * kEach / kCpc) + h) * kCpc + x * kEach % kCpc;
       u32x4 y;
-      if constexpr (kLook == kElements) {
-        const Piece<16> piece = element_piece<elem, 16>((const elem *)a.Q + (first_head + min(i, heads - 1)) * d, column, i < heads ? d : 0, false);
+      if constexpr (kLook >= kDwords) {
+        const Piece<16> piece = element_piece<elem, 16>((const elem *)a.Q + (first_head + min(i, heads - 1)) * d, column, i < heads ? d : 0);
         y = u32x4{piece.x[0], piece.x[1], piece.x[2], piece.x[3]};
       } else {
         y = buffer_load16(q, column < d ? (uint32_t)((i * d + column) * sizeof(elem)) : kPastEnd);
@@ -417,8 +430,6 @@ kernel(Args a) {
   // reads 7.0 TB/s so, 6.1 otherwise.  A line fetched in pieces would be fetched again: with rows of 160 bytes 250 us became 266.
   constexpr int kPolicyK = kLook == kWholeRows ? kOnce : 0, kPolicyV = kDh * kSize >= 128 ? kOnce : 0;
 
-  const bool dwords = kLook == kElements && (row_bytes & 3) == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0;
-
   typedef Piece<16> KPiece;
   typedef Piece<kVBytes> VPiece;
   KPiece kr[2][kKn];
@@ -459,7 +470,9 @@ kernel(Args a) {
           const int column = (8 * (x / 2) + k_chunk) * kCpc;
           // (columns that do not exist are loaded from the row's end; what is not q's to see is cleared before it is used)
           if constexpr (kLook == kElements) {
-            kr[s][x] = element_piece<cached, 16>((const cached *)row, column, d, dwords);
+            kr[s][x] = element_piece<cached, 16>((const cached *)row, column, d);
+          } else if constexpr (kLook == kDwords) {
+            kr[s][x] = last_piece<16>(row, column * kSize, (int)row_bytes);
           } else if (!half_chunk) {
             kr[s][x] = memory_piece<16>(row + min(column, d - kCpc) * kSize);
           } else {
@@ -495,7 +508,9 @@ kernel(Args a) {
 #pragma unroll
           for (int x = 0; x < kHf; ++x) {
             if constexpr (kLook == kElements)
-              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, d, dwords);
+              vr[4 * s + v][x] = element_piece<cached, kVBytes>((const cached *)row, (16 * x + i) * kVC, d);
+            else if constexpr (kLook == kDwords)
+              vr[4 * s + v][x] = last_piece<kVBytes>(row, (16 * x + i) * kVBytes, (int)row_bytes);
             else
               vr[4 * s + v][x] = memory_piece<kVBytes>(row + min((16 * x + i) * kVC, d - kVC) * kSize);
           }
@@ -537,6 +552,12 @@ kernel(Args a) {
     if constexpr (kQInLds) asm volatile("" ::: "memory");  // q is read within the loop
     // ---- S^T = K Q^T ----
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if constexpr (kLook == kDwords) {
+#pragma unroll
+      for (int x = 0; x < kKn; ++x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) move_down(kr[t][x], (8 * (x / 2) + k_chunk) * 16, (int)row_bytes);
+    }
     if constexpr (kLines) {
 #pragma unroll
       for (int x = 0; x < kKn; x += 2)
@@ -545,7 +566,7 @@ kernel(Args a) {
 #pragma unroll
           for (int w = 0; w < 4; ++w) own_row(kr[t][x].x[w], kr[t][x + 1].x[w]);
     }
-    if constexpr (kLook == kPerKey) {
+    if constexpr (kLook == kPerKey || kLook == kDwords) {
       if (d != kDh) {
 #pragma unroll
         for (int x = 0; x < kKn; ++x)
@@ -655,6 +676,12 @@ kernel(Args a) {
       for (int e = 0; e < 8; ++e) p[e] *= vsr[e >> 2][e & 3];
     }
     // ---- O^T += V^T P^T ----
+    if constexpr (kLook == kDwords) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int x = 0; x < kHf; ++x) move_down(vr[e][x], (16 * x + i) * kVBytes, (int)row_bytes);
+    }
     if constexpr (kF32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -753,7 +780,9 @@ template <class E, class C> void launch_cache(const Args &a, unsigned workgroups
   // whole 16-byte chunks of a row, 8 bytes at its end in an 8-bit cache
   constexpr int kSize = sizeof(typename C::elem), kEven = is_8bit<C>::value ? 8 : 16 / kSize;
   const bool chunks = a.d % kEven == 0 && (((uintptr_t)a.k | (uintptr_t)a.v) & (kEven * kSize - 1)) == 0 && ((uintptr_t)a.Q & 3) == 0;
-  if (!chunks) launch_look<E, C, kElements>(a, workgroups, stream);
+  const bool dwords = a.d * kSize % 4 == 0 && a.d * kSize >= 16 && (((uintptr_t)a.k | (uintptr_t)a.v) & 3) == 0;
+  if (!chunks && dwords) launch_look<E, C, kDwords>(a, workgroups, stream);
+  else if (!chunks) launch_look<E, C, kElements>(a, workgroups, stream);
   else if (a.map.page.d % 16 == 0 && (a.d == 64 || a.d == 128 || a.d == 256)) launch_look<E, C, kWholeRows>(a, workgroups, stream);
   else if (a.map.page.d % 16 == 0) launch_look<E, C, kInPage>(a, workgroups, stream);
   else launch_look<E, C, kPerKey>(a, workgroups, stream);

@@ -229,6 +229,28 @@ def test_long_sequences(dtype, lens, page, hq, hkv, d, kind):
     Setup(dtype, kind, hq, hkv, d, page, lens, seed=len(lens) + page).check()
 
 
+@pytest.mark.parametrize("dtype,kind,hq,hkv,d,page", [
+    ("f32", "plain", 4, 2, 33, 16), ("f32", "plain", 2, 2, 5, 4), ("f32", "plain", 3, 1, 66, 7), ("f32", "plain", 2, 1, 131, 16),
+    ("f32", "plain", 2, 1, 255, 8), ("f32", "i8", 4, 2, 100, 16), ("f32", "e4m3", 4, 2, 20, 1), ("f32", "i8", 2, 1, 252, 3),
+    ("f32", "e4m3", 2, 2, 60, 24), ("bf16", "plain", 4, 1, 42, 16), ("f16", "plain", 2, 2, 10, 5), ("bf16", "plain", 2, 1, 250, 16),
+    ("f16", "plain", 17, 1, 126, 3), ("bf16", "i8", 4, 1, 36, 16), ("f16", "e4m3", 2, 2, 124, 7), ("bf16", "e4m3", 2, 1, 244, 16),
+    ("f16", "i8", 2, 1, 28, 2), ("bf16", "i8", 3, 1, 12, 16), ("f16", "plain", 2, 1, 6, 16), ("f32", "plain", 2, 1, 3, 16)])
+def test_rows_that_end_inside_a_chunk(dtype, kind, hq, hkv, d, page):
+    Setup(dtype, kind, hq, hkv, d, page, [0, 1, 31, 33, 257, 700], seed=d).check()
+
+
+@pytest.mark.parametrize("dtype,kind,d,off", [("bf16", "plain", 128, 2), ("f32", "plain", 64, 1), ("f16", "i8", 128, 4), ("bf16", "e4m3", 256, 4),
+                                              ("f16", "plain", 64, 1), ("bf16", "i8", 64, 1)])
+def test_pages_at_odd_addresses(dtype, kind, d, off):
+    s = Setup(dtype, kind, 4, 2, d, 16, [130, 0, 77])
+    moved = []
+    for x in s.cache[:2]:
+        y = torch.zeros(x.numel() + off, dtype=x.dtype, device=DEV)[off:].view(x.shape)
+        moved.append(y.copy_(x))
+    s.cache = (*moved, *s.cache[2:])
+    s.check()
+
+
 @pytest.mark.parametrize("kind", ["plain", "i8"])
 def test_many_sequences(kind):
     """More sequences than a wave has lanes, than the chip has room for parts of."""
