@@ -11,9 +11,11 @@
 //   - O^T += V^T P^T: those 2 x 4 keys are k = 8 h + 0..7, so P^T needs no exchange between lanes.  Lane (i, h) loads columns
 //     8 i + 0..7 of its 8 keys (16 lanes together a whole row of 128 columns); the fragment of the m-th product, whose rows are the
 //     columns 8 i + m, is the m-th element of each of them: four byte permutations, half an instruction per element.
-// fp32 queries do both products with v_mfma_f32_16x16x4_f32, an element of a lane's chunk per step.
+// fp32 queries over a cache of fp32 do both products with v_mfma_f32_16x16x4_f32, an element of a lane's chunk per step; over 8 bits,
+// which are exact in bf16, queries and P are three bf16 parts each, 24 bits (30 sequences of 4000, 8 heads of 64, int8: 51 us with the
+// former, 29 so; of 256 261, 125).
 // Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  P enters the
-// matrix unit in two 16-bit parts (the second holds what the first cuts off, 2^-15 of P remain): the matrix unit is idle nine
+// matrix unit in two 16-bit parts for 16-bit queries (the second holds what the first cuts off, 2^-15 of P remain): the matrix unit is idle nine
 // tenths of the time, and the result is as exact as fp32 probabilities make it.
 //
 // Bound by memory: keys and values are read once, 2 d elements each key against 4 d flops per query head.  Measured, with the
@@ -131,7 +133,7 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma16(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// Four cached 8-bit elements (one dword) as 16-bit elements of E, two dwords, or as floats; all exact.
+// Four cached 8-bit elements (one dword) as 16-bit elements of E, two dwords; exact.
 __device__ __forceinline__ void widen(E4m3, Bf16, uint32_t x, uint32_t (&y)[2]) {
   y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
   y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true));
@@ -143,10 +145,6 @@ __device__ __forceinline__ void widen(E4m3, F16, uint32_t x, uint32_t (&y)[2]) {
 __device__ __forceinline__ void floats(I8, uint32_t x, float (&y)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(x >> (8 * e));
-}
-__device__ __forceinline__ void floats(E4m3, uint32_t x, float (&y)[4]) {
-  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
-  y[0] = a[0], y[1] = a[1], y[2] = b[0], y[3] = b[1];
 }
 __device__ __forceinline__ void widen(I8, Bf16, uint32_t x, uint32_t (&y)[2]) {
   float f[4];
@@ -180,6 +178,25 @@ __device__ __forceinline__ void two_parts(F16, const float (&p)[8], f16x8 &hi, f
     hi[e] = (_Float16)h[0], hi[e + 1] = (_Float16)h[1];
     lo[e] = (_Float16)fmaf(p[e], 0x1p-20f, p[e] - (float)h[0]);
     lo[e + 1] = (_Float16)fmaf(p[e + 1], 0x1p-20f, p[e + 1] - (float)h[1]);
+  }
+}
+// The same in three parts, all 24 bits, of fp32 probabilities against 8-bit values, and of fp32 queries (+-) against 8-bit keys; of
+// an infinity or a NaN the first is that and the others are 0.
+__device__ __forceinline__ void three_parts(const float (&p)[8], bf16x8 (&y)[3]) {
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = p[e];
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    u32x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * e + 1]), __float_as_uint(rest[2 * e]), 0x07060302u);
+    y[part] = as_x8<Bf16>(h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float cut = rest[e] - __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+      rest[e] = fabsf(p[e]) < INFINITY ? cut : 0.f;
+    }
   }
 }
 // P is kept this many powers of two above exp(S - maximum): fp16 has few exponents below 1.
@@ -329,6 +346,8 @@ kernel(Args a) {
   typedef typename std::conditional<kF32, Bf16, E>::type E16;
   typedef typename std::conditional<k8, Bf16, E16>::type P16;
   typedef typename P16::x8 px8;
+  constexpr bool kMat32 = kF32 && !k8;       // fp32 matrix instructions; 8-bit elements are exact in bf16, fp32 is three of them
+  constexpr int kParts = kF32 ? 3 : 1;       // of a query's element
   constexpr float kShift = kF32 ? 0.f : shift_log2<P16>::value;
 
   constexpr int kStride = 16 * kVC + 4;
@@ -357,6 +376,7 @@ kernel(Args a) {
   constexpr bool kQInLds = kDh == 256 ? !k8 : kDh == 128 && waves_per_simd<E, C>(kDh, kLook) == 4;
   __shared__ u32x4 q_lds[kQInLds ? kQn : 1][64];
   u32x4 q_reg[kQn];
+  bf16x8 q_parts[kF32 && k8 ? kQn / 2 : 1][kParts];  // of 8 columns, where they are three
   {
     const buffer_t q = make_buffer((const elem *)a.Q + first_head * d, (size_t)heads * d * sizeof(elem));  // no rows behind `heads`
 #pragma unroll
@@ -370,6 +390,15 @@ kernel(Args a) {
         y = buffer_load16(q, column < d ? (uint32_t)((i * d + column) * sizeof(elem)) : kPastEnd);
       }
       q_reg[x] = y;
+    }
+  }
+  if constexpr (kF32 && k8) {
+#pragma unroll
+    for (int x = 0; x < kQn; x += 2) {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(q_reg[x + e / 4][e % 4]);
+      three_parts(f, q_parts[x / 2]);
     }
   }
   auto q_at = [&](int x) {
@@ -581,15 +610,7 @@ kernel(Args a) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const KPiece &p = kr[t][x];
-        if constexpr (kF32 && k8) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            float f[4];
-            floats(C(), p.x[w], f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[t] = mfma16(f[e], __uint_as_float(q_at(4 * x + w)[e]), s[t]);
-          }
-        } else if constexpr (kF32) {
+        if constexpr (kMat32) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[t] = mfma16(__uint_as_float(p.x[e]), __uint_as_float(q_at(x)[e]), s[t]);
         } else if constexpr (k8) {
@@ -598,7 +619,13 @@ kernel(Args a) {
             uint32_t w0[2], w1[2];
             widen(C(), E16(), p.x[2 * y], w0);
             widen(C(), E16(), p.x[2 * y + 1], w1);
-            s[t] = mfma16(as_x8<E16>(u32x4{w0[0], w0[1], w1[0], w1[1]}), as_x8<E16>(q_at(2 * x + y)), s[t]);
+            const auto key = as_x8<E16>(u32x4{w0[0], w0[1], w1[0], w1[1]});
+            if constexpr (kF32) {
+#pragma unroll
+              for (int part = kParts - 1; part >= 0; --part) s[t] = mfma16(key, q_parts[2 * x + y][part], s[t]);
+            } else {
+              s[t] = mfma16(key, as_x8<E16>(q_at(2 * x + y)), s[t]);
+            }
           }
         } else {
           s[t] = mfma16(as_x8<E16>(u32x4{p.x[0], p.x[1], p.x[2], p.x[3]}), as_x8<E16>(q_at(x)), s[t]);
@@ -682,22 +709,17 @@ kernel(Args a) {
 #pragma unroll
         for (int x = 0; x < kHf; ++x) move_down(vr[e][x], (16 * x + i) * kVBytes, (int)row_bytes);
     }
-    if constexpr (kF32) {
+    if constexpr (kMat32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int x = 0; x < kHf; ++x) {
-          float f[4];
-          if constexpr (k8) floats(C(), vr[e][x].x[0], f);
-          else
+        for (int x = 0; x < kHf; ++x)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) f[m] = __uint_as_float(vr[e][x].x[m]);
-#pragma unroll
-          for (int m = 0; m < 4; ++m) acc[x][m] = mfma16(f[m], p[e], acc[x][m]);
-        }
+          for (int m = 0; m < 4; ++m) acc[x][m] = mfma16(__uint_as_float(vr[e][x].x[m]), p[e], acc[x][m]);
     } else {
-      px8 hi, lo;
-      two_parts(P16(), p, hi, lo);
+      px8 parts[kF32 ? 3 : 2];
+      if constexpr (kF32) three_parts(p, parts);
+      else two_parts(P16(), p, parts[0], parts[1]);
 #pragma unroll
       for (int x = 0; x < kHf; ++x) {
         uint32_t w[8][kVC / 2];  // columns in pairs
@@ -721,8 +743,8 @@ kernel(Args a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = __builtin_amdgcn_perm(w[2 * e + 1][m / 2], w[2 * e][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
           const px8 vf = as_x8<P16>(f);
-          acc[x][m] = mfma16(vf, lo, acc[x][m]);
-          acc[x][m] = mfma16(vf, hi, acc[x][m]);
+#pragma unroll
+          for (int part = (int)(sizeof(parts) / sizeof(px8)) - 1; part >= 0; --part) acc[x][m] = mfma16(vf, parts[part], acc[x][m]);
         }
       }
     }

@@ -239,6 +239,16 @@ def test_rows_that_end_inside_a_chunk(dtype, kind, hq, hkv, d, page):
     Setup(dtype, kind, hq, hkv, d, page, [0, 1, 31, 33, 257, 700], seed=d).check()
 
 
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 16), (100, 5), (128, 32), (33, 16), (256, 1)])
+def test_fp32_queries_of_many_magnitudes(d, page, kind):
+    """All bits of a query's element count: large ones that cancel, small ones beside them."""
+    s = Setup("f32", kind, 4, 2, d, page, [300, 40, 5], seed=3)
+    g = torch.Generator().manual_seed(4)
+    s.q *= (10 ** (torch.rand(s.q.shape, generator=g) * 6 - 5)).to(DEV)
+    s.check()
+
+
 @pytest.mark.parametrize("dtype,kind,d,off", [("bf16", "plain", 128, 2), ("f32", "plain", 64, 1), ("f16", "i8", 128, 4), ("bf16", "e4m3", 256, 4),
                                               ("f16", "plain", 64, 1), ("bf16", "i8", 64, 1)])
 def test_pages_at_odd_addresses(dtype, kind, d, off):
