@@ -33,6 +33,7 @@ constexpr int kUnit = kTile * kWaves;   // sequences are cut at multiples of thi
 constexpr int kHeads = 16;              // query heads of a workgroup
 constexpr int kMostUnits = 1 << 24;     // of the longest sequence, 2^31 tokens
 constexpr float kLazyLog2 = 8.f;
+constexpr float kMostFloat = 3.402823466e38f;
 
 // How the sequences are cut into parts, one workgroup's work per KV head: see find_part.
 struct Split {
@@ -673,7 +674,8 @@ kernel(Args a) {
     // ---- softmax ----
     float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     if (__any(mx > m_thr)) {
-      const float m_new = fmaxf(m_ref, head_max(mx));
+      // (finite: an infinite score then has the exponential infinity and not NaN, and so has LSE)
+      const float m_new = fminf(fmaxf(m_ref, head_max(mx)), kMostFloat);
       const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_ref - m_new) * a.scale_log2);
       l_run *= alpha;  // a NaN of before stays
 #pragma unroll
@@ -778,7 +780,7 @@ kernel(Args a) {
         sum += weight * part_l[w][head];
         o += weight * part_o[w][head][c];
       }
-      const float exponent = m * a.scale_log2 - kShift;
+      const float exponent = fminf(m * a.scale_log2 - kShift, kMostFloat);
       if (part.parts == 1) {
         ((elem *)a.O)[(first_head + head) * d + column] = (elem)(sum != 0.f ? o / sum : 0.f);
         if (column == 0)

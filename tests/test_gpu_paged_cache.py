@@ -242,11 +242,29 @@ def test_rows_that_end_inside_a_chunk(dtype, kind, hq, hkv, d, page):
 @pytest.mark.parametrize("kind", ["i8", "e4m3"])
 @pytest.mark.parametrize("d,page", [(64, 16), (100, 5), (128, 32), (33, 16), (256, 1)])
 def test_fp32_queries_of_many_magnitudes(d, page, kind):
-    """All bits of a query's element count: large ones that cancel, small ones beside them."""
+    """All bits of a query's element count: large ones that cancel, small ones beside them, and one that is not finite."""
     s = Setup("f32", kind, 4, 2, d, page, [300, 40, 5], seed=3)
     g = torch.Generator().manual_seed(4)
     s.q *= (10 ** (torch.rand(s.q.shape, generator=g) * 6 - 5)).to(DEV)
     s.check()
+    s.q[1, 2, 3], s.q[2, 0, 1] = float("nan"), float("inf")
+    o, lse = s.attend()
+    want, log = attend64(s.q, s.cache, s.table, s.lens)[:2]
+    assert torch.equal(torch.isnan(o.cpu()), torch.isnan(want)) and torch.equal(torch.isnan(lse.cpu()), torch.isnan(log))
+    assert int(torch.isnan(o).sum()) == 2 * d
+    assert torch.equal(lse.cpu() == float("inf"), log == float("inf"))
+
+
+@pytest.mark.parametrize("kind", ["plain", "i8"])
+@pytest.mark.parametrize("dtype,lens", [("bf16", [700, 3]), ("f16", [2500]), ("f32", [1500, 40])])
+def test_scores_of_infinity(dtype, lens, kind):
+    """O is NaN as softmax is, and LSE infinity, unless a score is NaN."""
+    s = Setup(dtype, kind, 4, 2, 64, 16, lens)
+    s.q[0, 0, 5], s.q[-1, 2, 7], s.q[-1, 3, 9] = float("inf"), -float("inf"), float("nan")
+    o, lse = s.attend()
+    want, log = attend64(s.q, s.cache, s.table, s.lens)[:2]
+    assert torch.equal(torch.isnan(o.cpu()), torch.isnan(want))
+    assert torch.equal(torch.isnan(lse.cpu()), torch.isnan(log)) and torch.equal(lse.cpu() == float("inf"), log == float("inf"))
 
 
 @pytest.mark.parametrize("dtype,kind,d,off", [("bf16", "plain", 128, 2), ("f32", "plain", 64, 1), ("f16", "i8", 128, 4), ("bf16", "e4m3", 256, 4),
