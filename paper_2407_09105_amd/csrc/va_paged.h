@@ -15,8 +15,9 @@
 // which are exact in bf16, queries and P are three bf16 parts each, 24 bits (30 sequences of 4000, 8 heads of 64, int8: 51 us with the
 // former, 29 so; of 256 261, 125).
 // Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  P enters the
-// matrix unit in two 16-bit parts for 16-bit queries (the second holds what the first cuts off, 2^-15 of P remain): the matrix unit is idle nine
-// tenths of the time, and the result is as exact as fp32 probabilities make it.
+// matrix unit in three bf16 parts, which hold all its 24 bits (over fp16 values in two fp16 parts, 22 bits), so that O is as exact as fp32
+// products make it: with two bf16 parts, 16 bits, one of some hundred 16-bit results was rounded the other way.  The matrix unit is idle
+// most of the time; the third part costs nothing that can be measured (16 sequences of up to 4000, 16 heads of 256: 109.5 us with two, 110 with three).
 //
 // Bound by memory: keys and values are read once, 2 d elements each key against 4 d flops per query head.  Measured, with the
 // joining: 131072 keys of 8 heads of 128 in bf16 87 us (6.1 TB/s; the kernel alone 6.6, the card reads 7.0), 128 sequences of
@@ -162,16 +163,8 @@ __device__ __forceinline__ void widen(I8, F16, uint32_t x, uint32_t (&y)[2]) {
   y[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u)) - off);
 }
 
-// P (>= 0) in two parts of 16 bits.  The first is cut off, not rounded, and the second holds the rest and 2^-20 more: positive like
-// P, so that an infinity in V comes out as one.
-__device__ __forceinline__ void two_parts(Bf16, const float (&p)[8], bf16x8 &hi, bf16x8 &lo) {
-  u32x4 h;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) lo[e] = (__bf16)fmaf(p[e], 0x1p-20f, p[e] - __uint_as_float(__float_as_uint(p[e]) & 0xffff0000u));
-#pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
-  hi = as_x8<Bf16>(h);
-}
+// P (>= 0) in two parts of fp16, against values of fp16.  The first is cut off, not rounded, and the second holds the rest and 2^-20
+// more: positive like P, so that an infinity in V comes out as one.
 __device__ __forceinline__ void two_parts(F16, const float (&p)[8], f16x8 &hi, f16x8 &lo) {
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
@@ -181,9 +174,11 @@ __device__ __forceinline__ void two_parts(F16, const float (&p)[8], f16x8 &hi, f
     lo[e + 1] = (_Float16)fmaf(p[e + 1], 0x1p-20f, p[e + 1] - (float)h[1]);
   }
 }
-// The same in three parts, all 24 bits, of fp32 probabilities against 8-bit values, and of fp32 queries (+-) against 8-bit keys; of
-// an infinity or a NaN the first is that and the others are 0.
-__device__ __forceinline__ void three_parts(const float (&p)[8], bf16x8 (&y)[3]) {
+// Numbers in three parts of bf16, all 24 bits: fp32 queries (+-) against 8-bit keys, and P (times the scale of V over 8 bits).  Each part is
+// cut off, not rounded; of an infinity or a NaN the first is that and the others are 0.
+// kPositive: P against values of bf16, which may be infinite: the later parts also hold 2^-30 of P, so that they are positive like P and an
+// infinity in V comes out as one (zero times it would be NaN).
+template <bool kPositive> __device__ __forceinline__ void three_parts(const float (&p)[8], bf16x8 (&y)[3]) {
   float rest[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) rest[e] = p[e];
@@ -196,7 +191,8 @@ __device__ __forceinline__ void three_parts(const float (&p)[8], bf16x8 (&y)[3])
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float cut = rest[e] - __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-      rest[e] = fabsf(p[e]) < INFINITY ? cut : 0.f;
+      if constexpr (kPositive) rest[e] = fmaf(p[e], 0x1p-30f, cut);
+      else rest[e] = fabsf(p[e]) < INFINITY ? cut : 0.f;
     }
   }
 }
@@ -349,6 +345,7 @@ kernel(Args a) {
   typedef typename P16::x8 px8;
   constexpr bool kMat32 = kF32 && !k8;       // fp32 matrix instructions; 8-bit elements are exact in bf16, fp32 is three of them
   constexpr int kParts = kF32 ? 3 : 1;       // of a query's element
+  constexpr int kPParts = std::is_same<P16, Bf16>::value ? 3 : 2;  // of a probability
   constexpr float kShift = kF32 ? 0.f : shift_log2<P16>::value;
 
   constexpr int kStride = 16 * kVC + 4;
@@ -399,7 +396,7 @@ kernel(Args a) {
       float f[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(q_reg[x + e / 4][e % 4]);
-      three_parts(f, q_parts[x / 2]);
+      three_parts<false>(f, q_parts[x / 2]);
     }
   }
   auto q_at = [&](int x) {
@@ -719,9 +716,10 @@ kernel(Args a) {
 #pragma unroll
           for (int m = 0; m < 4; ++m) acc[x][m] = mfma16(__uint_as_float(vr[e][x].x[m]), p[e], acc[x][m]);
     } else {
-      px8 parts[kF32 ? 3 : 2];
-      if constexpr (kF32) three_parts(p, parts);
-      else two_parts(P16(), p, parts[0], parts[1]);
+      px8 parts[kPParts];
+      if constexpr (kPParts == 3) three_parts<!k8>(p, parts);
+      else two_parts(F16(), p, parts[0], parts[1]);
+      __builtin_amdgcn_sched_barrier(0);  // values are waited for behind the softmax
 #pragma unroll
       for (int x = 0; x < kHf; ++x) {
         uint32_t w[8][kVC / 2];  // columns in pairs
@@ -746,7 +744,7 @@ kernel(Args a) {
           for (int e = 0; e < 4; ++e) f[e] = __builtin_amdgcn_perm(w[2 * e + 1][m / 2], w[2 * e][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
           const px8 vf = as_x8<P16>(f);
 #pragma unroll
-          for (int part = (int)(sizeof(parts) / sizeof(px8)) - 1; part >= 0; --part) acc[x][m] = mfma16(vf, parts[part], acc[x][m]);
+          for (int part = kPParts - 1; part >= 0; --part) acc[x][m] = mfma16(vf, parts[part], acc[x][m]);
         }
       }
     }

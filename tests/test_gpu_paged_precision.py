@@ -1,0 +1,93 @@
+"""How exactly attention over the key-value cache sums probabilities times values, seen where the sum cancels."""
+import math
+
+import pytest
+import torch
+
+from paper_2407_09105_amd import binding
+from tests.paged_util import CACHES, DEV, DTYPES, TOPS, attend64
+
+pytestmark = pytest.mark.gpu
+
+
+def _scores_in(t, x):
+    """Scores near x as the sum of two elements of type t, exact in fp32: (first, second, sum)."""
+    first = x.to(t).double()
+    second = (x - first).to(t).double()
+    return first, second, first + second
+
+
+def _worst_in_16_bits(p):
+    """Of p (float64) the two whose rounding to 16 significant bits changes them most, up and down: nearly 2^-16 of themselves.  (The ninth
+    bit is set, so that two parts of 8 bits are 16; none lies so near to a tie that the exponential's own error turns it over.)"""
+    step = torch.exp2(torch.floor(torch.log2(p)) - 15)
+    rest = p / step - torch.round(p / step)
+    worth = torch.where((torch.floor(p / step) % 256 >= 128) & (rest.abs() < 0.45), rest * step / p, 0.0)
+    assert worth.min() < -0.8 * 2.0 ** -16 and worth.max() > 0.8 * 2.0 ** -16
+    return int(worth.argmin()), int(worth.argmax())
+
+
+CANCELLING = [("bf16", "plain", 64, 16), ("bf16", "plain", 128, 16), ("bf16", "plain", 72, 16), ("bf16", "plain", 256, 5), ("bf16", "plain", 34, 16),
+              ("bf16", "plain", 33, 16), ("f16", "plain", 64, 16), ("f16", "plain", 128, 5), ("f16", "plain", 256, 16), ("f16", "plain", 33, 16),
+              ("bf16", "i8", 128, 16), ("bf16", "i8", 64, 5), ("f16", "i8", 128, 16), ("bf16", "e4m3", 128, 16), ("f16", "e4m3", 256, 16),
+              ("f16", "e4m3", 80, 24), ("f32", "plain", 64, 16), ("f32", "i8", 64, 16), ("f32", "e4m3", 128, 16)]
+
+
+@pytest.mark.parametrize("dtype,kind,d,page", CANCELLING)
+def test_probabilities_are_as_wide_as_fp32(dtype, kind, d, page):
+    """Keys 1 and 2 have probabilities (over 8 bits: products of them and the scale of V) whose bits behind the first 16 are worth nearly
+    2^-16 of them, one up and one down, and values of opposite signs; keys 3.. take away what is left of their sum, so that O is far smaller than its terms and the rounding of
+    the result with it.  Key 0 holds the maximum, 0, and has no value.
+
+    Off by, relative to A = sum_j P_j |v_j|: the exponent x = (S - max) log2 e, |x| <= X = 4 log2 e, is formed with three roundings, and a
+    fourth where an 8-bit key has a scale, 2^-24 X each and times ln 2 in P; the exponential 2^-22; P times the scale of V 2^-24; up to three
+    partial products for each of n keys and the four waves' results are added, 2^-23 of A each.  O is rounded once."""
+    hkv, n, t = 2, 10, DTYPES[dtype]
+    g = torch.Generator().manual_seed(d)
+    many = -(0.5 + 3.4 * torch.rand(20000, generator=g, dtype=torch.float64))
+    if kind == "plain":
+        first, second, many = _scores_in(t, many)
+    else:
+        many = -(-many / TOPS[kind]).float().double() * TOPS[kind]
+    used = [*_worst_in_16_bits(torch.exp(many))] + torch.randint(len(many), (n - 3,), generator=g).tolist()
+    S = torch.cat([torch.zeros(1, dtype=torch.float64), many[used]])
+    P = torch.exp(S)
+    width = -(-n // page)
+    k = torch.zeros((width, hkv, page, d), dtype=torch.float64)
+    v, ks, vs = torch.zeros_like(k), torch.ones(width, hkv, page), torch.ones(width, hkv, page)
+    left = torch.zeros((hkv, d), dtype=torch.float64)
+    for j in range(n):
+        at, row = j // page, j % page
+        if kind != "plain":
+            ks[at, :, row] = (-S[j] / TOPS[kind]).float()
+            k[at, :, row, 0] = -TOPS[kind]
+        elif j > 0:
+            k[at, :, row, 0], k[at, :, row, 1] = first[used[j - 1]], second[used[j - 1]]
+        want = (torch.zeros_like(left) if j == 0 else 1 + torch.rand((hkv, d), generator=g, dtype=torch.float64) if j == 1 else -left / P[j])
+        if kind == "plain":
+            v[at, :, row] = want = want.to(t).double()
+        else:
+            s = (want.abs().amax() / TOPS[kind]).float().expand(hkv)
+            if j in (1, 2):    # P and the scale are one factor: the product is what has to be wide
+                wider = s[0] * (1 + torch.rand(20000, generator=g))
+                s = wider[_worst_in_16_bits(P[j] * wider.double())[j - 1]].expand(hkv)
+            vs[at, :, row] = s
+            steps = want / torch.where(s > 0, s, 1.0).double()[:, None]
+            v[at, :, row] = steps = steps.round() if kind == "i8" else steps.float().to(CACHES[kind]).double()
+            want = steps * s.double()[:, None]
+        left += P[j] * want
+    elements = t if kind == "plain" else CACHES[kind]
+    scales = (None, None) if kind == "plain" else (ks.to(DEV), vs.to(DEV))
+    cache = (k.float().to(elements).to(DEV), v.float().to(elements).to(DEV), *scales)
+    q = torch.zeros((1, 2 * hkv, d), dtype=t)
+    q[:, :, :2] = 1     # scores are the sums of the keys' first two columns
+    q = q.to(DEV)
+    table, lens = torch.arange(width, dtype=torch.int32, device=DEV)[None], torch.tensor([n], dtype=torch.int32, device=DEV)
+    O, _, A, _ = attend64(q, cache, table, lens, 1.0)
+    assert (O.abs() < 2.0 ** -14 * A).all()
+    o, _ = binding.paged_attn_fwd(q, cache, table, lens, 1.0)
+    rel = 4 * 2.0 ** -24 * 4 + 2.0 ** -22 + 2.0 ** -24 + (3 * n + 4) * 2.0 ** -23
+    err = (o.cpu().double() - O).abs()
+    tol = A * rel + torch.finfo(t).eps / 2 * O.abs() + torch.finfo(t).smallest_normal * torch.finfo(t).eps
+    print("off by %.2e of the terms, tolerance %.2e" % (float((err / A).max()), rel))
+    assert (err <= tol).all(), float((err / tol).max())
