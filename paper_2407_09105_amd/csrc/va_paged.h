@@ -14,10 +14,14 @@
 // fp32 queries over a cache of fp32 do both products with v_mfma_f32_16x16x4_f32, an element of a lane's chunk per step; over 8 bits,
 // which are exact in bf16, queries and P are three bf16 parts each, 24 bits (30 sequences of 4000, 8 heads of 64, int8: 51 us with the
 // former, 29 so; of 256 261, 125).
-// Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  P enters the
-// matrix unit in three bf16 parts, which hold all its 24 bits (over fp16 values in two fp16 parts, 22 bits), so that O is as exact as fp32
-// products make it: with two bf16 parts, 16 bits, one of some hundred 16-bit results was rounded the other way.  The matrix unit is idle
-// most of the time; the third part costs nothing that can be measured (16 sequences of up to 4000, 16 heads of 256: 109.5 us with two, 110 with three).
+// Softmax: fp32, running maximum and sum per head, the maximum moved only when it grows by more than 2^kLazyLog2.  O is as exact as fp32
+// products make it, whatever the elements.  Against bf16 and 8-bit values P enters the matrix unit in three bf16 parts, which hold all its
+// 24 bits: with two, 16 bits, one of some hundred 16-bit results was rounded the other way.  The matrix unit is idle most of the time; the
+// third part costs nothing that can be measured (16 sequences of up to 4000, 16 heads of 256: 109.5 us with two, 110 with three).
+// fp16 has no room for P: two fp16 parts keep 22 bits of the largest and none of what lies 2^-31 below, of which a long context may be made.
+// fp16 values are widened instead, and O^T += V^T P^T runs in v_mfma_f32_16x16x4_f32, an element of a column per step: 131072 keys of 8
+// heads of 128 105 -> 109 us, 48 sequences of about 700 41.7 -> 44.3, 16 of up to 4000 with 16 heads of 256 110 -> 126.  Values in two bf16
+// parts against P in three would cost as much (108, 42.7, 127) and its registers spill.
 //
 // Bound by memory: keys and values are read once, 2 d elements each key against 4 d flops per query head.  Measured, with the
 // joining: 131072 keys of 8 heads of 128 in bf16 87 us (6.1 TB/s; the kernel alone 6.6, the card reads 7.0), 128 sequences of
@@ -163,17 +167,6 @@ __device__ __forceinline__ void widen(I8, F16, uint32_t x, uint32_t (&y)[2]) {
   y[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u)) - off);
 }
 
-// P (>= 0) in two parts of fp16, against values of fp16.  The first is cut off, not rounded, and the second holds the rest and 2^-20
-// more: positive like P, so that an infinity in V comes out as one.
-__device__ __forceinline__ void two_parts(F16, const float (&p)[8], f16x8 &hi, f16x8 &lo) {
-#pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    const auto h = __builtin_amdgcn_cvt_pkrtz(p[e], p[e + 1]);
-    hi[e] = (_Float16)h[0], hi[e + 1] = (_Float16)h[1];
-    lo[e] = (_Float16)fmaf(p[e], 0x1p-20f, p[e] - (float)h[0]);
-    lo[e + 1] = (_Float16)fmaf(p[e + 1], 0x1p-20f, p[e + 1] - (float)h[1]);
-  }
-}
 // Numbers in three parts of bf16, all 24 bits: fp32 queries (+-) against 8-bit keys, and P (times the scale of V over 8 bits).  Each part is
 // cut off, not rounded; of an infinity or a NaN the first is that and the others are 0.
 // kPositive: P against values of bf16, which may be infinite: the later parts also hold 2^-30 of P, so that they are positive like P and an
@@ -196,9 +189,6 @@ template <bool kPositive> __device__ __forceinline__ void three_parts(const floa
     }
   }
 }
-// P is kept this many powers of two above exp(S - maximum): fp16 has few exponents below 1.
-template <class E> struct shift_log2 { static constexpr float value = 0.f; };
-template <> struct shift_log2<F16> { static constexpr float value = 6.f; };
 
 // ---- the kernel ---------------------------------------------------------------------------------------
 
@@ -339,14 +329,10 @@ kernel(Args a) {
   constexpr int kCpc = 16 / kSize, kKn = kDh / (4 * kCpc);
   // V: kVC columns of a row for a lane at a time, kHf times
   constexpr int kVC = kF32 || kDh == 64 ? 4 : 8, kHf = kDh / (16 * kVC), kVBytes = kVC * kSize;
-  // matrix operands: of the queries' type, but P goes with 8-bit values as bf16, which has the range for their scales
-  typedef typename std::conditional<kF32, Bf16, E>::type E16;
-  typedef typename std::conditional<k8, Bf16, E16>::type P16;
-  typedef typename P16::x8 px8;
-  constexpr bool kMat32 = kF32 && !k8;       // fp32 matrix instructions; 8-bit elements are exact in bf16, fp32 is three of them
-  constexpr int kParts = kF32 ? 3 : 1;       // of a query's element
-  constexpr int kPParts = std::is_same<P16, Bf16>::value ? 3 : 2;  // of a probability
-  constexpr float kShift = kF32 ? 0.f : shift_log2<P16>::value;
+  typedef typename std::conditional<kF32, Bf16, E>::type E16;  // matrix operands of S over 16 and 8 bits
+  // fp32 matrix instructions: S of fp32 alone, O also of fp16, whose range small probabilities leave
+  constexpr bool kMat32 = kF32 && !k8, kMat32V = !k8 && !std::is_same<C, Bf16>::value;
+  constexpr int kParts = kF32 ? 3 : 1;       // of a query's element over 8 bits
 
   constexpr int kStride = 16 * kVC + 4;
   __shared__ __attribute__((aligned(16))) float part_o[kWaves][kHeads][kStride];
@@ -686,7 +672,7 @@ kernel(Args a) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3] - base, a.scale_log2, kShift));
+      p[e] = __builtin_amdgcn_exp2f((s[e >> 2][e & 3] - base) * a.scale_log2);
       l_run += p[e];
     }
     if constexpr (k8) {
@@ -708,17 +694,24 @@ kernel(Args a) {
 #pragma unroll
         for (int x = 0; x < kHf; ++x) move_down(vr[e][x], (16 * x + i) * kVBytes, (int)row_bytes);
     }
-    if constexpr (kMat32) {
+    if constexpr (kMat32V) {
+      if constexpr (kSize == 2) __builtin_amdgcn_sched_barrier(0);  // values are waited for behind the softmax
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int x = 0; x < kHf; ++x)
 #pragma unroll
-          for (int m = 0; m < 4; ++m) acc[x][m] = mfma16(__uint_as_float(vr[e][x].x[m]), p[e], acc[x][m]);
+          for (int w = 0; w < kVBytes / 4; ++w) {
+            struct Columns { cached x[4 / kSize]; };
+            uint32_t two = vr[e][x].x[w];
+            if constexpr (kSize == 2) asm("" : "+v"(two));  // converted here, not where the word comes from, which would take twice its registers
+            const Columns c = __builtin_bit_cast(Columns, two);
+#pragma unroll
+            for (int m = 0; m < 4 / kSize; ++m) acc[x][w * 4 / kSize + m] = mfma16((float)c.x[m], p[e], acc[x][w * 4 / kSize + m]);
+          }
     } else {
-      px8 parts[kPParts];
-      if constexpr (kPParts == 3) three_parts<!k8>(p, parts);
-      else two_parts(F16(), p, parts[0], parts[1]);
+      bf16x8 parts[3];
+      three_parts<!k8>(p, parts);
       __builtin_amdgcn_sched_barrier(0);  // values are waited for behind the softmax
 #pragma unroll
       for (int x = 0; x < kHf; ++x) {
@@ -729,7 +722,7 @@ kernel(Args a) {
 #pragma unroll
             for (int y = 0; y < kVC / 4; ++y) {
               uint32_t two[2];
-              widen(C(), P16(), vr[e][x].x[y], two);
+              widen(C(), Bf16(), vr[e][x].x[y], two);
               w[e][2 * y] = two[0], w[e][2 * y + 1] = two[1];
             }
           } else {
@@ -742,9 +735,9 @@ kernel(Args a) {
           u32x4 f;
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = __builtin_amdgcn_perm(w[2 * e + 1][m / 2], w[2 * e][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
-          const px8 vf = as_x8<P16>(f);
+          const bf16x8 vf = as_x8<Bf16>(f);
 #pragma unroll
-          for (int part = kPParts - 1; part >= 0; --part) acc[x][m] = mfma16(vf, parts[part], acc[x][m]);
+          for (int part = 2; part >= 0; --part) acc[x][m] = mfma16(vf, parts[part], acc[x][m]);
         }
       }
     }
@@ -778,7 +771,7 @@ kernel(Args a) {
         sum += weight * part_l[w][head];
         o += weight * part_o[w][head][c];
       }
-      const float exponent = fminf(m * a.scale_log2 - kShift, kMostFloat);
+      const float exponent = fminf(m * a.scale_log2, kMostFloat);
       if (part.parts == 1) {
         ((elem *)a.O)[(first_head + head) * d + column] = (elem)(sum != 0.f ? o / sum : 0.f);
         if (column == 0)

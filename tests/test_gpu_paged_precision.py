@@ -91,3 +91,41 @@ def test_probabilities_are_as_wide_as_fp32(dtype, kind, d, page):
     tol = A * rel + torch.finfo(t).eps / 2 * O.abs() + torch.finfo(t).smallest_normal * torch.finfo(t).eps
     print("off by %.2e of the terms, tolerance %.2e" % (float((err / A).max()), rel))
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype,kind,d,page,n", [("f16", "plain", 64, 16, 20000), ("f16", "plain", 128, 16, 9000), ("f16", "plain", 40, 24, 300),
+                                                 ("f16", "plain", 33, 16, 9000), ("f16", "plain", 256, 32, 9000), ("f16", "i8", 64, 16, 9000),
+                                                 ("f16", "e4m3", 128, 5, 9000), ("bf16", "plain", 64, 16, 9000), ("bf16", "i8", 64, 16, 300)])
+@pytest.mark.parametrize("below", [12.0, 16.0, 18.0, 20.0, 22.0, 26.0])
+def test_probabilities_far_below_the_largest(dtype, kind, d, page, n, below):
+    """One key holds nearly all of the softmax and no value; the others, equal ones some nats below it, are all that O is made of.  Each
+    is as exact as one near the largest.
+
+    Relative to O (all terms have one sign): the exponent x = below log2 e, formed with four roundings of 2^-24 x; the exponential 2^-22; P
+    times V's scale 2^-24; sums in fp32, of at most 75 keys in a wave (parts of 256 keys, or 300 uncut) and then of the waves and n / 256 parts,
+    2^-23 each.  O is rounded once."""
+    t, width = DTYPES[dtype], -(-n // page)
+    g = torch.Generator().manual_seed(int(below))
+    k, v = torch.zeros((width, 1, page, d)), torch.randint(1, 16, (width, 1, page, d), generator=g).float()
+    at, row = n // 2 // page, n // 2 % page
+    v[at, 0, row] = 0.0
+    if kind == "plain":
+        k[at, 0, row, 0] = below
+        cache = (k.to(t).to(DEV), (v * 2048).to(t).to(DEV), None, None)
+    else:
+        k[at, 0, row, 0] = TOPS[kind]
+        ks, vs = torch.ones((width, 1, page)), torch.full((width, 1, page), 2048.0)
+        ks[at, 0, row] = below / TOPS[kind]
+        cache = (k.to(CACHES[kind]).to(DEV), v.to(CACHES[kind]).to(DEV), ks.to(DEV), vs.to(DEV))
+    q = torch.zeros((1, 2, d), dtype=t, device=DEV)
+    q[:, :, 0] = 1
+    table, lens = torch.arange(width, dtype=torch.int32, device=DEV)[None], torch.tensor([n], dtype=torch.int32, device=DEV)
+    O, LSE, _, _ = attend64(q, cache, table, lens, 1.0)
+    o, lse = binding.paged_attn_fwd(q, cache, table, lens, 1.0)
+    fi = torch.finfo(t)
+    rel = 4 * 2.0 ** -24 * below + 2.0 ** -22 + 2.0 ** -24 + (75 + 4 + n / 256) * 2.0 ** -23
+    tol = (rel + fi.eps / 2) * O.abs() + fi.smallest_normal * fi.eps / 2
+    err = (o.cpu().double() - O).abs()
+    print("off by %.2e of O, tolerance %.2e" % (float((err / O).max()), rel + fi.eps / 2))
+    assert (err <= tol).all(), float((err / tol).max())
+    assert ((lse.cpu().double() - LSE).abs() <= 2.0 ** -22 * LSE.abs() + rel).all()
