@@ -48,8 +48,8 @@ struct Split {
 };
 Split split_of(int n_seqs, long long capacity, int hq, int hkv);
 
-// Of every sequence where its parts begin and how many it has; then of all parts in order [slots, hq] pairs (reference exponent,
-// sum of P) and [slots, hq, d] sums of P V.
+// Of every sequence where its parts begin and how many it has; then of all parts in order [slots, hq] pairs (reference score before it
+// is scaled, sum of P) and [slots, hq, d] sums of P V.
 struct Workspace {
   int2 *parts;
   float2 *ml;
@@ -214,8 +214,14 @@ struct Args {
   Workspace ws;
   FastDiv hkv, groups;  // KV heads; groups of kHeads query heads of one KV head
   int hq, G, d;         // G = hq / hkv
-  float scale_log2;
+  float scale, scale_log2;
 };
+
+// log sum exp(S) of a row from its reference score and the sum of P.  (Scores are scaled on their own: as exponents of two the
+// largest would pass fp32's range, by 1.44.)
+__device__ __forceinline__ float lse_of(float m, float sum, float scale) {
+  return sum != 0.f ? fmaf(m, scale, log2f(sum) * 0.6931471805599453f) : -INFINITY;
+}
 
 // Between lanes 8 apart in a row of 16 (i and i + 8): before, lane l holds a of row l % 8 and b of row 8 + l % 8; after, the lower
 // lane both a's of its row, its own and the upper one's, and the upper lane both b's, the lower one's first.
@@ -771,15 +777,13 @@ kernel(Args a) {
         sum += weight * part_l[w][head];
         o += weight * part_o[w][head][c];
       }
-      const float exponent = fminf(m * a.scale_log2, kMostFloat);
       if (part.parts == 1) {
         ((elem *)a.O)[(first_head + head) * d + column] = (elem)(sum != 0.f ? o / sum : 0.f);
-        if (column == 0)
-          a.LSE[(size_t)(g * G + head0 + head) * map.n_seqs + b] = sum != 0.f ? (exponent + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        if (column == 0) a.LSE[(size_t)(g * G + head0 + head) * map.n_seqs + b] = lse_of(m, sum, a.scale);
       } else {
         const size_t to = (size_t)slot * a.hq + g * G + head0 + head;
         a.ws.o[to * d + column] = o;
-        if (column == 0) a.ws.ml[to] = make_float2(exponent, sum);
+        if (column == 0) a.ws.ml[to] = make_float2(m, sum);
       }
     }
   }

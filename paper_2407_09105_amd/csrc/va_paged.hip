@@ -33,13 +33,13 @@ Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
 
 namespace {
 
-// One workgroup per (sequence, query head) adds up the parts' sums, weighted relative to the largest reference exponent: every
+// One workgroup per (sequence, query head) adds up the parts' sums, weighted relative to the largest reference score: every
 // kJoinRows-th part one group of threads', a column each, and then the groups' sums in order.
 constexpr int kMostParts = kWorkgroups + kMoreWorkgroups + 1;  // of one sequence
 
 template <class E, int kCols>  // kCols: threads of a group, d rounded up to 64, 128 or 256
 __global__ void __launch_bounds__(kThreads)
-join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d) {
+join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d, float scale, float scale_log2) {
   constexpr int kJoinRows = kThreads / kCols, kFly = 8;  // parts in flight
   __shared__ float weight[kMostParts], some[2][kThreads];
   const int b = blockIdx.x, head = blockIdx.y, t = threadIdx.x;
@@ -72,7 +72,7 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
 #pragma unroll
   for (int k = 0; k * kThreads < kMostParts; ++k) {
     const int x = t + k * kThreads;
-    const float w = mine[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[k].x - top);
+    const float w = mine[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[k].x - top) * scale_log2);
     if (x < parts) weight[x] = w;
     sum += w * mine[k].y;
   }
@@ -97,14 +97,14 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
     for (int k = 0; k < kJoinRows; ++k) y += some[0][k * kCols + c];
   }
   if (t < d) O[((size_t)b * hq + head) * d + t] = (typename E::elem)(sum != 0.f ? y / sum : 0.f);
-  if (t == 0) LSE[(size_t)head * n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  if (t == 0) LSE[(size_t)head * n_seqs + b] = lse_of(top, sum, scale);
 }
 
 // The same by one wave per (sequence, query head), four of them in a workgroup, for batches in which a sequence has few parts: a
 // column per lane and 64 of d, the weights of 64 parts at a time in the lanes.
 template <class E, int kCols>
 __global__ void __launch_bounds__(kThreads)
-join_few_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d) {
+join_few_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace ws, int n_seqs, int hq, int d, float scale, float scale_log2) {
   constexpr int kOwn = kCols / 64, kFly = 4;
   const int b = blockIdx.x, head = blockIdx.y * kWaves + uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (head >= hq) return;
@@ -121,7 +121,7 @@ join_few_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Works
   for (int x0 = 0; x0 < parts; x0 += 64) {
     const int x = x0 + lane;
     const float2 one = x < parts ? ml[(size_t)x * hq] : make_float2(-INFINITY, 0.f);
-    const float weight = one.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(one.x - top);
+    const float weight = one.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((one.x - top) * scale_log2);
     sum += weight * one.y;
     const int many = min(parts - x0, 64);
     for (int k0 = 0; k0 < many; k0 += kFly) {
@@ -144,22 +144,23 @@ join_few_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Works
 #pragma unroll
   for (int e = 0; e < kOwn; ++e)
     if (lane + 64 * e < d) O[((size_t)b * hq + head) * d + lane + 64 * e] = (typename E::elem)(sum != 0.f ? y[e] / sum : 0.f);
-  if (lane == 0) LSE[(size_t)head * n_seqs + b] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  if (lane == 0) LSE[(size_t)head * n_seqs + b] = lse_of(top, sum, scale);
 }
 
-template <class E> void launch_join(void *O, float *LSE, const Workspace &ws, const Split &split, int n_seqs, int hq, int d, hipStream_t stream) {
+template <class E> void launch_join(void *O, float *LSE, const Workspace &ws, const Split &split, int n_seqs, int hq, int d, float scale,
+                                    float scale_log2, hipStream_t stream) {
   const dim3 grid((unsigned)n_seqs, (unsigned)hq);
   typename E::elem *const o = (typename E::elem *)O;
   if ((int)split.extra.d <= kFewParts * n_seqs) {
     const dim3 few((unsigned)n_seqs, (unsigned)ceil_div(hq, kWaves));
-    if (d <= 64) join_few_kernel<E, 64><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
-    else if (d <= 128) join_few_kernel<E, 128><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
-    else join_few_kernel<E, 256><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+    if (d <= 64) join_few_kernel<E, 64><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
+    else if (d <= 128) join_few_kernel<E, 128><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
+    else join_few_kernel<E, 256><<<few, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
     return;
   }
-  if (d <= 64) join_kernel<E, 64><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
-  else if (d <= 128) join_kernel<E, 128><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
-  else join_kernel<E, 256><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d);
+  if (d <= 64) join_kernel<E, 64><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
+  else if (d <= 128) join_kernel<E, 128><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
+  else join_kernel<E, 256><<<grid, kThreads, 0, stream>>>(o, LSE, ws, n_seqs, hq, d, scale, scale_log2);
 }
 
 }  // namespace
@@ -175,14 +176,15 @@ hipError_t launch_paged(const void *Q, void *O, float *LSE, va_dtype dt, const v
   const Split split = split_of(c.n_seqs, (long long)c.max_pages * c.page_size, hq, c.hkv);
   const Workspace ws = workspace(work, split, c.n_seqs, hq);
   const int G = hq / c.hkv, groups = ceil_div(G, kHeads);
-  const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, fast_div(c.hkv), fast_div(groups), hq, G, c.d,
+  const Args a = {Q, O, LSE, c.k, c.v, c.k_scale, c.v_scale, page_map(c), lens, split, ws, fast_div(c.hkv), fast_div(groups), hq, G, c.d, scale,
                   scale * 1.4426950408889634f};
   const long long workgroups = ((long long)split.slots * c.hkv + 7) / 8 * 8 * groups;
   if (workgroups > kMostWorkgroups) return hipErrorInvalidValue;
   (dt == VA_BF16 ? launch_bf16 : dt == VA_F16 ? launch_f16 : launch_f32)(a, c.format, (unsigned)workgroups, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || split.slots == c.n_seqs) return e;
-  (dt == VA_BF16 ? launch_join<Bf16> : dt == VA_F16 ? launch_join<F16> : launch_join<F32>)(O, LSE, ws, split, c.n_seqs, hq, c.d, stream);
+  (dt == VA_BF16 ? launch_join<Bf16> : dt == VA_F16 ? launch_join<F16> : launch_join<F32>)(O, LSE, ws, split, c.n_seqs, hq, c.d, scale,
+                                                                                            a.scale_log2, stream);
   return hipGetLastError();
 }
 

@@ -129,3 +129,45 @@ def test_probabilities_far_below_the_largest(dtype, kind, d, page, n, below):
     print("off by %.2e of O, tolerance %.2e" % (float((err / O).max()), rel + fi.eps / 2))
     assert (err <= tol).all(), float((err / tol).max())
     assert ((lse.cpu().double() - LSE).abs() <= 2.0 ** -22 * LSE.abs() + rel).all()
+
+
+@pytest.mark.parametrize("dtype,kind,lens", [("bf16", "plain", [40, 9]), ("bf16", "plain", [3000, 700]), ("f32", "plain", [3000, 2]), ("f32", "i8", [40, 2600]),
+                                             ("bf16", "plain", [150000])])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_scores_near_the_types_limits(dtype, kind, lens, sign):
+    """Scores of 1 and 0.9 times the largest bf16 number, of either sign and in sequences that are cut or are not: the larger ones share the
+    softmax, the others have nothing of it, and LSE is that score (the logarithm of some thousand changes nothing)."""
+    t, page, d, n_pages = DTYPES[dtype], 16, 64, sum(-(-n // 16) for n in lens)
+    width = max(-(-n // page) for n in lens)
+    g = torch.Generator().manual_seed(len(lens))
+    big = torch.finfo(torch.bfloat16).max
+    less = float(torch.tensor(0.9 * big).bfloat16())
+    high, low = sign * (big if sign > 0 else less), sign * (less if sign > 0 else big)
+    k, v = torch.zeros((n_pages, 1, page, d)), torch.randint(-8, 9, (n_pages, 1, page, d), generator=g).float()
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(lens):
+        table[b, :-(-n // page)] = torch.arange(at, at + -(-n // page))
+        at += -(-n // page)
+    scores = torch.full((n_pages, page), high)
+    scores[::3] = low       # pages of the smaller scores, the first of them among these
+    scales = (None, None)
+    if kind == "plain":
+        k[:, 0, :, 0] = scores
+    else:
+        k[:, 0, :, 0] = 1.0 if sign > 0 else -1.0
+        scales = (scores.abs()[:, None].contiguous().to(DEV), torch.ones(n_pages, 1, page, device=DEV))
+    elements = t if kind == "plain" else CACHES[kind]
+    cache = (k.to(elements).to(DEV), v.to(elements).to(DEV), *scales)
+    q = torch.zeros((len(lens), 2, d), dtype=t, device=DEV)
+    q[:, :, 0] = 1
+    given = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    o, lse = binding.paged_attn_fwd(q, cache, table.to(DEV), given, 1.0)
+    for b, n in enumerate(lens):
+        rows = v[table[b, :-(-n // page)].long(), 0].reshape(-1, d)[:n].double()
+        mine = scores[table[b, :-(-n // page)].long()].reshape(-1)[:n]
+        top = float(mine.max())
+        want = rows[mine == top].mean(0)
+        # whole numbers below 2^21 are added exactly; the sum of the weights (ones) too; one division and one rounding
+        assert ((o[b].cpu().double() - want).abs() <= (torch.finfo(t).eps / 2 + 2.0 ** -22) * want.abs()).all()
+        assert ((lse[:, b].cpu().double() - top).abs() <= 2.0 ** -23 * abs(top)).all()
