@@ -1,9 +1,9 @@
-"""The key-value cache at sizes that take more than one launch."""
+"""The key-value cache at sizes that take more than one launch, more parts than a wave has lanes or a workgroup threads."""
 import pytest
 import torch
 
 from paper_2407_09105_amd import binding
-from tests.paged_util import DEV
+from tests.paged_util import DEV, Setup
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,25 @@ def test_rows_of_more_than_one_launch(d, kind, tokens):
     del stored, pages, rows
     out = binding.paged_cache_read(cache, table, token, seq)
     assert torch.equal(out[0], k) and torch.equal(out[1], v)
+
+
+@pytest.mark.parametrize("d", [40, 128, 200])
+def test_one_sequence_of_more_parts_than_a_workgroup_has_threads(d):
+    """80000 keys for one head: 313 parts of 256."""
+    Setup("bf16", "plain", 1, 1, d, 64, [80000], seed=d, garbage=False).check()
+
+
+@pytest.mark.parametrize("kind", ["plain", "i8"])
+def test_a_long_sequence_among_empty_ones(kind):
+    """64 sequences for one head may have 768 more parts than one each, and one of them has 651 of three times 128 keys."""
+    lens = [0] * 64
+    lens[3], lens[40] = 17, 249_900
+    Setup("f16", kind, 2, 1, 16, 256, lens, seed=5, garbage=False).check()
+
+
+@pytest.mark.parametrize("d,hq", [(64, 1), (96, 3), (256, 5)])
+def test_a_long_sequence_among_many_short_ones(d, hq):
+    """300 sequences have room for fewer than eight parts each; one of them has 79."""
+    lens = [(13 * b) % 50 for b in range(300)]
+    lens[170] = 20_000
+    Setup("bf16", "plain", hq, 1, d, 16, lens, seed=d, garbage=False).check()
