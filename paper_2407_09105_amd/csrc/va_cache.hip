@@ -17,7 +17,6 @@ namespace va {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSpread = 64;  // groups of tokens that are spread well enough over the 8 XCDs, whole groups at a time
 
 __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) {
   return it == VA_I64 ? (long long)((const int64_t *)ids)[t] : (long long)((const int32_t *)ids)[t];
@@ -27,9 +26,9 @@ __device__ __forceinline__ long long id_at(const void *ids, va_itype it, int t) 
 // kLanes = 0: d / kVec lanes, whatever that is; no lane idles, but a row cannot be reduced across its lanes (head_dim 96 of 8 heads,
 // 8300 e4m3 tokens read 12.5 -> 10.3 us).
 // kPast: stores of whole 128-byte lines pass by the caches (non-temporal; lines that two workgroups share would be written twice):
-// 65536 tokens of 8 heads of 128 written behind a rotary embedding of K 152 -> 128 us, read back 211 -> 193, and 2 to 3 % slower to 8 % faster
-// together with the next reader of the rows.  Loads do not: the rows to be written have often just left another kernel (16384 of
-// those tokens behind the embedding 35 us, with such loads 38).
+// 65536 bf16 tokens of 8 heads of 128: K's rotary embedding and the write 149 -> 135 us, the read alone 105 -> 95, write and read
+// together 205 -> 193; 2 to 3 % slower to 8 % faster together with the next reader of the rows.  Loads do not: the rows to be written have
+// often just left another kernel (16384 of those tokens behind the embedding 35 us, with such loads 38).
 template <class E, class C, int kVec, int kLanes, bool kWhole>
 struct Row {
   typedef typename E::elem elem;
@@ -100,17 +99,18 @@ struct Row {
 // What a thread works on: kItems rows of K and of V, their loads and look-ups in flight together, and its place in them.  A group of
 // tokens has as many workgroups as there are heads, which take one head each (neighbours in a page, and in K and V where a row is
 // whole lines), or, kInOrder, an equal part of the group's rows in the order of K and V, so that lines that rows share are stored
-// by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 -> 190 us, e4m3 rows of 96 85 -> 81.  together: the workgroups of a
+// by one workgroup: int8 rows of 80, 32 heads, 49152 tokens read 245 -> 190 us, e4m3 rows of 96 85 -> 81.  kTogether: the workgroups of a
 // group on one XCD, whose L2 then serves both that share a line (60000 tokens of 32 heads of 80 written: bf16 into pages of 16 252 ->
-// 240 us, pages of one 363 -> 248, int8 there 336 -> 291; 8300 e4m3 rows of 8 heads of 96 read 10.4 -> 9.4, fp32 rows of 33 110 -> 103).
-template <int kLanes, int kItems, bool kInOrder> struct Work {
+// 240 us, pages of one 363 -> 248, int8 there 336 -> 291; 8300 e4m3 rows of 8 heads of 96 read 10.4 -> 9.4, fp32 rows of 33 110 -> 103),
+// also where few groups leave XCDs out (32 heads of 80 quantised: 400 tokens 6.4 -> 5.5, 200 of 4 heads 4.0 and 4.0).
+template <int kLanes, int kItems, bool kInOrder, bool kTogether> struct Work {
   int lane, t[kItems], g[kItems];  // token, head
   bool there[kItems];
-  __device__ __forceinline__ Work(int first, int N, const FastDiv &heads, const FastDiv &lanes, bool together) {
+  __device__ __forceinline__ Work(int first, int N, const FastDiv &heads, const FastDiv &lanes) {
     const int H = heads.d, tid = threadIdx.x, per_row = kLanes ? kLanes : (int)lanes.d, rows = kThreads / per_row;
     const int mine = kLanes ? tid / (kLanes ? kLanes : 1) : tid / lanes;  // row of this thread
     int group = (int)blockIdx.x / heads, head = (blockIdx.x - group * H + group) % heads;  // heads in turn across XCDs
-    if (together) {
+    if constexpr (kTogether) {
       const int turn = blockIdx.x >> 3, eighth = turn / heads;
       group = eighth * 8 + (blockIdx.x & 7), head = turn - eighth * H;
     }
@@ -134,12 +134,11 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 write_kernel(const typename E::elem *__restrict__ K, const typename E::elem *__restrict__ V, typename C::elem *__restrict__ Kc,
              typename C::elem *__restrict__ Vc, float *__restrict__ ks, float *__restrict__ vs, PageMap map,
-             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d,
-             bool together) {
+             const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   constexpr bool kPast = kWhole && sizeof(typename C::elem) * kVec * kLanes % 128 == 0;
   const int H = heads.d;
-  const Work<kLanes, kItems, false> work(first, N, heads, lanes, together);
+  const Work<kLanes, kItems, false, !kWhole> work(first, N, heads, lanes);
   const int lane = work.lane;
   typename E::elem k[kItems][R::kPer], v[kItems][R::kPer];
   int place[kItems];
@@ -175,12 +174,11 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(typename E::elem *__restrict__ K, typename E::elem *__restrict__ V, const typename C::elem *__restrict__ Kc,
             const typename C::elem *__restrict__ Vc, const float *__restrict__ ks, const float *__restrict__ vs, PageMap map,
-            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d,
-            bool together) {
+            const int32_t *__restrict__ seq_ids, const void *__restrict__ pos, va_itype it, int first, int N, FastDiv heads, FastDiv lanes, int d) {
   typedef Row<E, C, kVec, kLanes, kWhole> R;
   constexpr bool kInOrder = kLanes == 0, kPast = kInOrder ? kVec > 1 : sizeof(typename E::elem) * kVec * kLanes % 128 == 0;
   const int H = heads.d;
-  const Work<kLanes, kItems, kInOrder> work(first, N, heads, lanes, together);
+  const Work<kLanes, kItems, kInOrder, !kWhole> work(first, N, heads, lanes);
   const int lane = work.lane;
   typename C::elem k[kItems][R::kPer], v[kItems][R::kPer];
   float sk[kItems], sv[kItems];
@@ -240,19 +238,18 @@ template <class E, class C, int kVec, int kLanes, bool kWhole, int kItems> hipEr
   for (long long first = 0; first < a.N; first += most) {
     const long long end = std::min(first + most, (long long)a.N);
     long long groups = (end - first + rows - 1) / rows;
-    const bool together = !kWhole && groups >= kSpread;
-    if (together) groups = (groups + 7) / 8 * 8;
+    if (!kWhole) groups = (groups + 7) / 8 * 8;  // a group of each XCD at a time
     const unsigned workgroups = (unsigned)(groups * a.c.hkv);
     if constexpr (kWrites)
       if (a.write)
         write_kernel<E, C, kVec, kLanes, kWhole, kItems><<<workgroups, kThreads, 0, a.stream>>>(
             (const elem *)a.K, (const elem *)a.V, (cached *)a.c.k, (cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-            (int)first, (int)end, heads, lanes, a.c.d, together);
+            (int)first, (int)end, heads, lanes, a.c.d);
     if constexpr (kReads)
       if (!a.write)
         read_kernel<E, C, kVec, kLanes, kWhole, kItems><<<workgroups, kThreads, 0, a.stream>>>(
             (elem *)a.K, (elem *)a.V, (const cached *)a.c.k, (const cached *)a.c.v, a.c.k_scale, a.c.v_scale, map, a.seq_ids, a.pos, a.it,
-            (int)first, (int)end, heads, lanes, a.c.d, together);
+            (int)first, (int)end, heads, lanes, a.c.d);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
