@@ -445,8 +445,10 @@ kernel(Args a) {
 #pragma unroll
   for (int x = 0; x < kHf; ++x) v_off[x] = (16 * x + i) * kVC < d ? (uint32_t)(4 * h * row_bytes + (16 * x + i) * kVBytes) : kPastEnd;
   const bool half_chunk = k8 && (d & 8) != 0;  // rows end in the middle of a 16-byte chunk
-  // Rows are read once and pass by the caches' other contents (non-temporal loads) where a load takes whole 128-byte lines: this card
-  // reads 7.0 TB/s so, 6.1 otherwise.  A line fetched in pieces would be fetched again: with rows of 160 bytes 250 us became 266.
+  // Rows pass by the caches (non-temporal loads) where a load takes whole 128-byte lines: this card reads 7.0 TB/s so, 6.1 otherwise (64
+  // sequences of 4096, 32 / 8 heads of 128, 192 us without and 171 so).  Right where rows are read once, and kept where they are not: if
+  // those sequences share half their pages 126 and 120; 15 of 16 pages 90 and 102; and with 64 query heads to each of two KV heads, whose keys
+  // four workgroups read, 104 and 132.  A line fetched in pieces would be fetched again: with rows of 160 bytes 250 us became 266.
   constexpr int kPolicyK = kLook == kWholeRows ? kOnce : 0, kPolicyV = kDh * kSize >= 128 ? kOnce : 0;
 
   typedef Piece<16> KPiece;

@@ -12,12 +12,17 @@ namespace paged {
 // 85 us with either, but 8.7 or 5.8 for the joining; 4 x 30000 of 2 heads of 256 60 us in all with 1024 and 50 with 512.  Sequences
 // of different lengths leave their last parts, which finer ones even out: 128 of 1024 to 8192 tokens, 8 heads, 232 us with 1024 and
 // 220 with 2048, 33 of 4096, 32 heads of 64, 227 and 213; 4096 gain nothing more.
+// At most kMorePerPair of the additional ones for each sequence and KV head: 8 sequences of 1024 to 16384, 8 heads, 59.5, 56.6, 53.6 and 57.3 us
+// with 1, 2, 4 and 8; 48 of about 700 40.3, 38.7, 37.6 and 37.8; 131072 keys, whose parts are equal anyway, 88 with 4 and 103 with 8.
 constexpr int kWorkgroups = 512, kMoreWorkgroups = 1536, kMorePerPair = 4;
+// Least units of a part (of one, two and four): 1500 keys, 8 heads of 128, 10.1, 11.3 and 14.1 us; 4 sequences of 500 to 2000 12.1, 12.2 and 15.1; 20
+// of up to 2500, 4 int8 heads of 80, 18.3, 15.4 and 16.4; 33 of up to 3001, one int8 head of 64, 13.7, 14 and 16.8.
 constexpr int kLeastUnits = 2;
 constexpr int kUncut = 512;    // sequences times KV heads that fill the chip in one piece each
-// Up to this many parts a sequence on average are joined by one wave for each head: 128 sequences, 40 heads, two parts 10.9 -> 4.8 us,
-// 3 sequences of up to eight 3.9 -> 3.4; with 128 parts (one sequence) a workgroup takes 9 us.
-constexpr int kFewParts = 8;
+// Up to this much room for more parts than one of each sequence (the host does not know how many there are), parts are joined by one wave
+// for each head: 128 sequences, 40 heads, two parts 10.9 -> 4.8 us, 3 sequences of up to eight 3.9 -> 3.4; with 128 parts (one
+// sequence) a workgroup takes 9 us.
+constexpr int kFewParts = 8;   // a sequence
 
 Split split_of(int n_seqs, long long capacity, int hq, int hkv) {
   const int groups = ceil_div(hq / hkv, kHeads);
@@ -100,7 +105,7 @@ join_kernel(typename E::elem *__restrict__ O, float *__restrict__ LSE, Workspace
   if (t == 0) LSE[(size_t)head * n_seqs + b] = lse_of(top, sum, scale);
 }
 
-// The same by one wave per (sequence, query head), four of them in a workgroup, for batches in which a sequence has few parts: a
+// The same by one wave per (sequence, query head), four of them in a workgroup, for batches in which there is room for few parts a sequence: a
 // column per lane and 64 of d, the weights of 64 parts at a time in the lanes.
 template <class E, int kCols>
 __global__ void __launch_bounds__(kThreads)
