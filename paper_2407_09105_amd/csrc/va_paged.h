@@ -387,7 +387,7 @@ kernel(Args a) {
     for (int x = 0; x < kQn; x += 2) {
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(q_reg[x + e / 4][e % 4]);
+      for (int e = 0; e < 8; ++e) f[e] = __builtin_canonicalizef(__uint_as_float(q_reg[x + e / 4][e % 4]));  // a NaN's first part shall be one
       three_parts<false>(f, q_parts[x / 2]);
     }
   }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2407_09105_amd import binding
-from tests.paged_util import CACHES, DEV, DTYPES, TOPS, attend64
+from tests.paged_util import CACHES, DEV, DTYPES, TOPS, Setup, attend64
 
 pytestmark = pytest.mark.gpu
 
@@ -171,3 +171,14 @@ def test_scores_near_the_types_limits(dtype, kind, lens, sign):
         # whole numbers below 2^21 are added exactly; the sum of the weights (ones) too; one division and one rounding
         assert ((o[b].cpu().double() - want).abs() <= (torch.finfo(t).eps / 2 + 2.0 ** -22) * want.abs()).all()
         assert ((lse[:, b].cpu().double() - top).abs() <= 2.0 ** -23 * abs(top)).all()
+
+
+@pytest.mark.parametrize("kind", ["plain", "i8", "e4m3"])
+@pytest.mark.parametrize("bits", [0x7f800001, -0x7fffff, 0x7fc00000])
+def test_nan_in_a_query_whatever_its_bits(kind, bits):
+    """Of some NaNs only the last of the 24 bits tells them from infinity."""
+    s = Setup("f32", kind, 2, 1, 64, 16, [40, 700])
+    s.q.view(torch.int32)[:, 1, 3] = bits
+    o, lse = s.attend()
+    assert torch.isnan(o[:, 1]).all() and torch.isnan(lse[1]).all()
+    assert torch.isfinite(o[:, 0]).all() and torch.isfinite(lse[0]).all()
