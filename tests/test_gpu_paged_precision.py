@@ -182,3 +182,22 @@ def test_nan_in_a_query_whatever_its_bits(kind, bits):
     o, lse = s.attend()
     assert torch.isnan(o[:, 1]).all() and torch.isnan(lse[1]).all()
     assert torch.isfinite(o[:, 0]).all() and torch.isfinite(lse[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("below", [1.0, 20.0, 40.0, 60.0])
+def test_infinite_values_of_small_probabilities(dtype, below):
+    """An infinity in V comes out as one however little its key weighs, as long as it weighs anything; its sign and column are kept."""
+    t = DTYPES[dtype]
+    k, v = torch.zeros((4, 1, 16, 64)), torch.ones((4, 1, 16, 64))
+    k[:, :, :, 0] = -below
+    k[0, 0, 3, 0] = 0.0       # the key that holds the softmax
+    v[1, 0, 5, 9], v[3, 0, 15, 40] = math.inf, -math.inf
+    q = torch.zeros((1, 2, 64), dtype=t, device=DEV)
+    q[:, :, 0] = 1
+    table, lens = torch.arange(4, dtype=torch.int32, device=DEV)[None], torch.tensor([64], dtype=torch.int32, device=DEV)
+    o, lse = binding.paged_attn_fwd(q, (k.to(t).to(DEV), v.to(t).to(DEV), None, None), table, lens, 1.0)
+    assert (o[0, :, 9] == math.inf).all() and (o[0, :, 40] == -math.inf).all() and torch.isfinite(lse).all()
+    others = torch.ones(64, dtype=torch.bool)
+    others[[9, 40]] = False
+    assert ((o[0][:, others.to(DEV)].float() - 1).abs() <= 2.0 ** -20).all()
