@@ -247,8 +247,8 @@ va_status va_varlen_attn_bwd_stages(const void *dO, const void *Q, const void *K
  *   page_table       : device, [n_seqs] rows of max_pages int32, table_stride entries apart: position p of sequence s lies in
  *                      page page_table[s * table_stride + p / page_size], at place p % page_size.  An entry outside
  *                      [0, n_pages) is no page; sequences may share pages.
- * Limits: n_pages * hkv * page_size < 2^31 (rows of one tensor), max_pages * page_size <= 2^31 - 2^10,
- * page_size * d < 2^26, n_seqs <= 65535.
+ * Limits: n_pages * hkv * page_size < 2^31 (rows of one tensor), max_pages * page_size <= 2^31 - 2^10, page_size * d < 2^26
+ * (VA_ERR_SHAPE); d <= 256, hkv <= 65535, n_seqs <= 65535 (VA_ERR_UNSUPPORTED).
  */
 typedef enum {
   VA_CACHE_PLAIN = 0, /* elements of the type that the call names for K and V (or Q)            */
@@ -300,9 +300,12 @@ va_status va_cache_read(void *K, void *V, va_dtype dt, const va_kv_cache *cache,
  *   softmax_scale : <= 0 means 1 / sqrt(d).
  *   workspace     : >= va_paged_attn_workspace_bytes(...) bytes, 16-byte aligned (may be NULL when that is 0): sums of the parts
  *                   that long sequences are cut into.  Calls that overlap in time need one each.
- * P V is summed in fp32 before it is divided by the sum of P: elements of V whose n-fold exceeds 10^36 may overflow to infinity.
- * n_seqs * hkv * ceil(hq / hkv / 16) > 2^23: VA_ERR_UNSUPPORTED.
- * The parts follow from the lengths alone and are joined in order: results are deterministic (no atomics).
+ * Arithmetic: products and sums in fp32, probabilities with all their 24 bits whatever `dt` and the cache's format, O rounded once.  P V
+ * is summed before it is divided by the sum of P: elements of V whose n-fold exceeds 10^36 may overflow to infinity.  A key that scores
+ * -infinity weighs nothing; where all do, nothing is left.
+ * hq > 65535, or n_seqs * hkv * ceil(hq / hkv / 16) > 2^23: VA_ERR_UNSUPPORTED.
+ * The parts follow from the call's shapes and lengths alone and are joined in order: results are deterministic (no atomics), but a
+ * sequence's last bits may depend on how many others the call has, how long they are, and how far the table reaches.
  */
 size_t va_paged_attn_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t page_size, int32_t hq, int32_t hkv, int32_t d);
 va_status va_paged_attn_fwd(const void *Q, void *O, float *LSE, va_dtype dt, const va_kv_cache *cache, int32_t hq,
