@@ -1,4 +1,5 @@
-"""How exactly attention over the key-value cache sums probabilities times values, seen where the sum cancels."""
+"""How exactly attention over the key-value cache sums probabilities times values: where the sum cancels, far below the largest
+probability, at scores near the types' limits and with values that are not finite."""
 import math
 
 import pytest
@@ -36,8 +37,8 @@ CANCELLING = [("bf16", "plain", 64, 16), ("bf16", "plain", 128, 16), ("bf16", "p
 @pytest.mark.parametrize("dtype,kind,d,page", CANCELLING)
 def test_probabilities_are_as_wide_as_fp32(dtype, kind, d, page):
     """Keys 1 and 2 have probabilities (over 8 bits: products of them and the scale of V) whose bits behind the first 16 are worth nearly
-    2^-16 of them, one up and one down, and values of opposite signs; keys 3.. take away what is left of their sum, so that O is far smaller than its terms and the rounding of
-    the result with it.  Key 0 holds the maximum, 0, and has no value.
+    2^-16 of them, one up and one down, and values of opposite signs; keys 3.. take away what is left of their sum, so that O is far
+    smaller than its terms and the rounding of the result with it.  Key 0 holds the maximum, 0, and has no value.
 
     Off by, relative to A = sum_j P_j |v_j|: the exponent x = (S - max) log2 e, |x| <= X = 4 log2 e, is formed with three roundings, and a
     fourth where an 8-bit key has a scale, 2^-24 X each and times ln 2 in P; the exponential 2^-22; P times the scale of V 2^-24; up to three
